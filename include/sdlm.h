@@ -19,7 +19,8 @@
  * sdlm_block_attn_masked_prefix (the noise-block rows and the causal rows of parallel training,
  * Sec. 3.3), sdlm_causal_attn (those causal rows as one call with 128-row query tiles), sdlm_linear / sdlm_linear3 / sdlm_linear_rmsnorm / sdlm_rmsnorm / sdlm_rope_block(2) / sdlm_swiglu /
  * sdlm_accept_commit_layers (the rest of a decoder layer of the Qwen-2.5 backbone, Sec. 4.1, for
- * whole-model steps), sdlm_lmhead_confidence_static (no workspace scratch),
+ * whole-model steps), sdlm_qk_norm_rope / sdlm_tree_attn / sdlm_sample / sdlm_tree_commit(_layers) (verification of a
+ * drafted tree, with sampled tokens), sdlm_kv_gather_batch, sdlm_lmhead_confidence_static (no workspace scratch),
  * sdlm_selftest_bounded_wait, options and counters.
  *
  * Conventions that hold for every call unless stated otherwise
@@ -456,6 +457,118 @@ sdlm_status sdlm_rope_block(sdlm_ctx* ctx, int32_t batch, int32_t D, const int32
 sdlm_status sdlm_rope_block2(sdlm_ctx* ctx, int32_t batch, int32_t D, const int32_t* seq_ids, int32_t n_heads, void* x,
                              int32_t n_heads2, void* x2, float theta, void* stream);
 sdlm_status sdlm_swiglu(sdlm_ctx* ctx, int32_t rows, int32_t I, const void* gate_up, void* out, void* stream);
+
+/* ---- verification of a drafted tree -- Sec. 3.4 (self-speculative decoding) for several drafted continuations at
+ * once.  The n <= 64 nodes of sequence b's tree are drafted tokens; node j hangs from node parent[b, j] < j, or from
+ * the cached history (any value that is not an earlier node, -1 say).  n_nodes: device int32 [batch], how many of the
+ * n rows sequence b has (clipped to 0..n), or NULL for n; rows behind them are padding, neither read nor written.
+ * The calls of a pass: sdlm_qk_norm_rope with each node's depth as its position, sdlm_tree_attn in every layer,
+ * sdlm_sample (or sdlm_lmhead_confidence) for the token that follows each node, sdlm_tree_commit(_layers).
+ *
+ * Conventions of these calls beyond those above: the context's device has to be the current one (INVALID_ARG
+ * otherwise); a slot number in seq_ids outside 0..max_batch-1 sets the device status DEVICE_CHECK and leaves the
+ * outputs of its rows as they are. */
+
+/* Rotary positions.  Pair i of a head's first rot_dim elements turns by position * f_i, f_i = theta^(-2i / rot_dim):
+ *   SDLM_ROPE_PLAIN  as it is;   SDLM_ROPE_LINEAR  f_i / factor;
+ *   SDLM_ROPE_NTK    theta * factor^(rot_dim / (rot_dim - 2)) in place of theta;
+ *   SDLM_ROPE_YARN   f_i / factor * r_i + f_i (1 - r_i), r_i = clamp((i - lo) / (hi - lo), 0, 1), with lo (hi) the
+ *                    pair that turns beta_fast (beta_slow) times within trained_len positions, rounded down (up):
+ *                    rot_dim ln(trained_len / (2 pi beta)) / (2 ln theta), held within 0..rot_dim-1; cosine and sine
+ *                    are multiplied by 0.1 ln(factor) + 1 when factor > 1.
+ * interleaved 0: pair i is elements i and i + rot_dim/2 (rotate-half), 1: elements 2i and 2i + 1.
+ * rot_dim: a multiple of 16, 0 = head_dim; elements beyond it are not rotated.  attn_factor > 0 replaces the factor on
+ * cosine and sine (0: as above, 1 for all but YARN). */
+typedef enum sdlm_rope_scaling { SDLM_ROPE_PLAIN = 0, SDLM_ROPE_LINEAR = 1, SDLM_ROPE_NTK = 2, SDLM_ROPE_YARN = 3 } sdlm_rope_scaling;
+typedef struct sdlm_rope {
+  float theta;          /* > 1                                     */
+  int32_t rot_dim;
+  int32_t interleaved;
+  int32_t scaling;      /* sdlm_rope_scaling                       */
+  float factor;         /* > 0; not looked at with SDLM_ROPE_PLAIN */
+  int32_t trained_len;  /* these three: SDLM_ROPE_YARN only        */
+  float beta_fast;
+  float beta_slow;
+  float attn_factor;
+} sdlm_rope;
+
+/* ---- rotary positions of query and key rows, with the RMS norm of every head in the same pass (beside
+ * sdlm_rope_block, which rotates whole heads at the positions behind the cached history):
+ *   y = x / sqrt(mean(x^2) + eps) * weight  per head (y = x without a weight),  out = y rotated as above.
+ * q [batch, D, n_heads, d] with q_stride elements from one of its batch * D rows to the next (at least n_heads * d, a
+ * multiple of 8: the rows may lie inside a stacked q/k/v product); k [batch, D, n_heads2, d] likewise; n_heads2 = 0
+ * leaves k out.  q_weight, k_weight: device bf16 [d], either may be NULL.  q_out / k_out: dense rows; either may be
+ * its own input when that is dense (in place), no other overlap.  positions: device int32 [batch, D] or NULL for
+ * 0..D-1 in every sequence; relative != 0, or positions NULL: counted from the length of slot seq_ids[b] (or b) as the
+ * tables stand on the stream, else absolute (batch may then exceed max_batch).  Positions may repeat and be negative.
+ * Angles are formed in 64 bits; arithmetic fp32 with one rounding to bf16 at the end.
+ * Errors: INVALID_ARG, SHAPE (batch beyond max_batch where slots are read), UNSUPPORTED (rot_dim % 16), CUDA. */
+sdlm_status sdlm_qk_norm_rope(sdlm_ctx* ctx, int32_t batch, int32_t D, const int32_t* seq_ids, const int32_t* positions,
+                              int32_t relative, const sdlm_rope* rope, float eps, int32_t n_heads, const void* q,
+                              int64_t q_stride, const void* q_weight, void* q_out, int32_t n_heads2, const void* k,
+                              int64_t k_stride, const void* k_weight, void* k_out, void* stream);
+
+/* ---- attention of a drafted tree over the paged cache:
+ *   out[b,j,h,:] = softmax_t( q[b,j,h,:] . K_t * scale ) V_t,  t over the slot's cached tokens (all visible), the
+ *   nodes on the path of node j and j itself.
+ * q, out [batch, n, Hq, d]; k_tree / v_tree [batch, n, Hkv, d]: device bf16; parent device int32 [batch, n].
+ * 1 <= n <= 64; any Hq/Hkv; max_block does not limit n.  n = 1 is attention of a single token.  Slots may repeat.
+ * K and V of the tree's nodes have to be finite.  fp32 scores, sums and accumulation, weights rounded to bf16 before
+ * they meet V, bf16 output; results do not depend on timing.  The cache is not modified.
+ * Uses workspace scratch: calls on one context must not overlap on the GPU.
+ * Errors: INVALID_ARG, SHAPE (batch, n, or a schedule beyond 32 bits), UNSUPPORTED (softmax_scale not positive), CUDA. */
+sdlm_status sdlm_tree_attn(sdlm_ctx* ctx, int32_t batch, int32_t n, const int32_t* seq_ids, const int32_t* n_nodes,
+                           const int32_t* parent, const void* q, const void* k_tree, const void* v_tree, void* out,
+                           void* stream);
+
+/* ---- acceptance of a drafted tree and commit of its accepted path (beside sdlm_verify_commit, which takes one chain).
+ * Node 0 is the last known token and is always accepted (its parent is not looked at); from an accepted node i the walk
+ * goes on to the lowest-numbered child whose draft_token equals next_token[b, i], the token decided on behind node i.
+ * draft_token, next_token, parent: device int32 [batch, n].  path [batch, n] (device int32, required): the accepted
+ * nodes in order, -1 behind them; accepted_len[b] = their number (at least 1; 0 without nodes); out_tokens [batch, n]:
+ * next_token of the path's nodes, -1 behind them; rows path[b, 0..accepted_len[b]) of k_tree / v_tree
+ * [batch, n, Hkv, d] are appended to the cache as sdlm_accept_commit appends its rows.  A sequence that fails
+ * commits nothing: accepted_len[b] = -1, its out_tokens are -1.
+ * The _layers form commits into several caches (as sdlm_accept_commit_layers; distinct contexts).
+ * Uses workspace scratch of the (first) context.
+ * Errors: as sdlm_accept_commit(_layers); n <= 64.  Device status: OUT_OF_PAGES, DEVICE_CHECK (also for a slot that
+ * the call names twice: both rows are refused). */
+sdlm_status sdlm_tree_commit(sdlm_ctx* ctx, int32_t batch, int32_t n, const int32_t* seq_ids, const int32_t* n_nodes,
+                             const int32_t* parent, const int32_t* draft_token, const int32_t* next_token,
+                             const void* k_tree, const void* v_tree, int32_t* accepted_len, int32_t* out_tokens,
+                             int32_t* path, void* stream);
+sdlm_status sdlm_tree_commit_layers(sdlm_ctx* const* ctxs, int32_t n_layers, int32_t batch, int32_t n,
+                                    const int32_t* seq_ids, const int32_t* n_nodes, const int32_t* parent,
+                                    const int32_t* draft_token, const int32_t* next_token, const void* const* k_tree,
+                                    const void* const* v_tree, int32_t* accepted_len, int32_t* out_tokens, int32_t* path,
+                                    void* stream);
+
+/* SDLM_KV_GATHER for several slots in one launch: k_out / v_out [batch, length, Hkv, d] (device bf16) receive the first
+ * `length` tokens of slot seq_ids[b] (or b); rows at or beyond a slot's length are left untouched.
+ * Errors: INVALID_ARG, SHAPE. */
+sdlm_status sdlm_kv_gather_batch(sdlm_ctx* ctx, int32_t batch, int32_t length, const int32_t* seq_ids, void* k_out,
+                                 void* v_out, void* stream);
+
+/* ---- sampling from logits (beside sdlm_lmhead_confidence, which decodes greedily without storing them).  For each
+ * row l of `logits` [rows, vocab], row_stride elements (>= vocab) from one row to the next, bf16 or float:
+ *   z = (l - max l) / temperature,  w = e^z;  in the order (l descending, index ascending)
+ *   top_k   keeps the first top_k (<= 0 or >= vocab: all);
+ *   top_p   of those the shortest prefix whose weight reaches top_p of theirs, at least one (>= 1: all);
+ *   min_p   of those the tokens with w >= min_p, at least the first (<= 0: all; the largest w is 1);
+ *   token = the lowest index whose cumulative kept weight, by index, exceeds u * W, W the kept tokens' weight;
+ *   prob = w[token] / W;  entropy = -sum (w/W) ln (w/W) in nats;  n_kept = number of tokens kept.
+ * temperature <= 0 (or NaN): greedy, the first token of the order.  -inf and NaN logits are never kept; +inf counts as
+ * the type's largest finite value; a row with nothing left gives token -1, prob 0, entropy 0, n_kept 0.
+ * u float [rows] in [0, 1); temperature, top_p, min_p float [rows], top_k int32 [rows]: device, each of the four may
+ * be NULL (1, all, all, all).  token int32, prob / entropy float [rows]: device, required, as sdlm_accept_commit takes
+ * them; n_kept int32 [rows] or NULL.  logits: aligned to its type (16-byte rows are read faster).
+ * Weights are formed in 64 bits and summed exactly: results do not depend on timing.  No workspace scratch.
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (vocab > 262144), CUDA. */
+typedef enum sdlm_logit_type { SDLM_LOGITS_BF16 = 0, SDLM_LOGITS_F32 = 1 } sdlm_logit_type;
+sdlm_status sdlm_sample(sdlm_ctx* ctx, int32_t rows, int32_t vocab, sdlm_logit_type type, const void* logits,
+                        int64_t row_stride, const float* u, const float* temperature, const int32_t* top_k,
+                        const float* top_p, const float* min_p, int32_t* token, float* prob, float* entropy,
+                        int32_t* n_kept, void* stream);
 
 /* Tuning / test knobs (the paper has no counterpart).  SDLM_OPT_LMHEAD_KERNEL: which stripe kernel
  * sdlm_lmhead_confidence uses: 0 = chosen from the shape (default), 1 = warp-level mma.sync

@@ -29,6 +29,9 @@ OPT_ATTN_EARLY_PREFETCH = 5
 OPT_HOST_HIDDEN_BY_ATTN = 6
 OPT_HOST_INPLACE_MAX_KB = 7
 
+ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_YARN = range(4)
+LOGITS_BF16, LOGITS_F32 = 0, 1
+
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "SHAPE", 3: "UNSUPPORTED", 4: "OUT_OF_PAGES", 5: "CUDA",
                 6: "TIMEOUT", 7: "DEVICE_CHECK", 8: "WORKSPACE"}
 
@@ -38,7 +41,8 @@ EXPORTED = ["sdlm_pool_bytes", "sdlm_workspace_bytes", "sdlm_create", "sdlm_dest
             "sdlm_block_attn_masked", "sdlm_verify_commit", "sdlm_accept_commit_carry",
             "sdlm_block_attn_verify", "sdlm_block_attn_carry", "sdlm_causal_attn",
             "sdlm_linear", "sdlm_linear3", "sdlm_linear3_rope", "sdlm_rmsnorm", "sdlm_rope_block", "sdlm_swiglu", "sdlm_selftest_bounded_wait", "sdlm_rope_block2", "sdlm_accept_commit_layers", "sdlm_block_attn_prefix", "sdlm_linear_swiglu",
-            "sdlm_block_attn_masked_prefix", "sdlm_linear_rmsnorm"]
+            "sdlm_block_attn_masked_prefix", "sdlm_linear_rmsnorm", "sdlm_qk_norm_rope", "sdlm_tree_attn",
+            "sdlm_tree_commit", "sdlm_tree_commit_layers", "sdlm_kv_gather_batch", "sdlm_sample"]
 
 
 def accept_commit_layers(contexts, tau: float, token, p_top1, entropy, k_blks, v_blks, accepted_len, out_tokens,
@@ -55,6 +59,26 @@ def accept_commit_layers(contexts, tau: float, token, p_top1, entropy, k_blks, v
         _ptr(_dev(p_top1, torch.float32, "p_top1")), _ptr(_dev(entropy, torch.float32, "entropy")), k_arr, v_arr,
         _ptr(_dev(accepted_len, torch.int32, "accepted_len")), _ptr(_dev(out_tokens, torch.int32, "out_tokens")),
         _stream_ptr(stream)))
+
+
+def tree_commit_layers(contexts, draft_token, next_token, parent, k_trees, v_trees, n_nodes=None, accepted_len=None,
+                       out_tokens=None, path=None, seq_ids=None, stream=None):
+    """sdlm_tree_commit_layers: one pass over the trees commits the accepted paths into every layer's cache."""
+    sd0 = contexts[0]
+    n_layers = len(contexts)
+    if len(k_trees) != n_layers or len(v_trees) != n_layers:
+        raise ValueError("k_trees and v_trees must hold one tensor per context")
+    for k, v in zip(k_trees, v_trees):
+        sd0._check_tree(parent, n_nodes, seq_ids, k=(k, "k_tree"), v=(v, "v_tree"))
+    accepted_len, out_tokens, path = sd0._tree_outputs(parent, draft_token, next_token, accepted_len, out_tokens, path)
+    ctx_arr = (C.c_void_p * n_layers)(*[c.ctx.value for c in contexts])
+    k_arr = (C.c_void_p * n_layers)(*[_ptr(t) for t in k_trees])
+    v_arr = (C.c_void_p * n_layers)(*[_ptr(t) for t in v_trees])
+    sd0._check("sdlm_tree_commit_layers", sd0.lib.sdlm_tree_commit_layers(
+        ctx_arr, n_layers, int(parent.shape[0]), int(parent.shape[1]), _ptr(seq_ids), _ptr(n_nodes), _ptr(parent),
+        _ptr(draft_token), _ptr(next_token), k_arr, v_arr, _ptr(accepted_len), _ptr(out_tokens), _ptr(path),
+        _stream_ptr(stream)))
+    return accepted_len, out_tokens, path
 
 
 class SdlmError(RuntimeError):
@@ -80,6 +104,30 @@ class _KvResult(C.Structure):
     _fields_ = [("page_table", C.c_void_p), ("seq_len", C.c_void_p), ("free_list", C.c_void_p),
                 ("free_head", C.c_void_p), ("free_tail", C.c_void_p), ("device_status", C.c_void_p),
                 ("table_bytes", C.c_size_t)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("theta", C.c_float), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("scaling", C.c_int32),
+                ("factor", C.c_float), ("trained_len", C.c_int32), ("beta_fast", C.c_float), ("beta_slow", C.c_float),
+                ("attn_factor", C.c_float)]
+
+
+@dataclass
+class RopeConfig:
+    """Rotary positions of sdlm_qk_norm_rope (struct sdlm_rope)."""
+    theta: float = 1000000.0
+    rot_dim: int = 0
+    interleaved: bool = False
+    scaling: int = ROPE_PLAIN
+    factor: float = 1.0
+    trained_len: int = 32768
+    beta_fast: float = 32.0
+    beta_slow: float = 1.0
+    attn_factor: float = 0.0
+
+    def to_c(self) -> _Rope:
+        return _Rope(self.theta, self.rot_dim, int(self.interleaved), int(self.scaling), self.factor, self.trained_len,
+                     self.beta_fast, self.beta_slow, self.attn_factor)
 
 
 @dataclass
@@ -168,6 +216,20 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.sdlm_rope_block2.argtypes = [vp, i32, i32, vp, i32, vp, i32, vp, f32, vp]
     lib.sdlm_swiglu.restype = C.c_int
     lib.sdlm_swiglu.argtypes = [vp, i32, i32, vp, vp, vp]
+    i64 = C.c_int64
+    lib.sdlm_qk_norm_rope.restype = C.c_int
+    lib.sdlm_qk_norm_rope.argtypes = [vp, i32, i32, vp, vp, i32, C.POINTER(_Rope), f32, i32, vp, i64, vp, vp, i32, vp, i64,
+                                      vp, vp, vp]
+    lib.sdlm_tree_attn.restype = C.c_int
+    lib.sdlm_tree_attn.argtypes = [vp, i32, i32] + [vp] * 8
+    lib.sdlm_tree_commit.restype = C.c_int
+    lib.sdlm_tree_commit.argtypes = [vp, i32, i32] + [vp] * 11
+    lib.sdlm_tree_commit_layers.restype = C.c_int
+    lib.sdlm_tree_commit_layers.argtypes = [vp, i32, i32, i32] + [vp] * 11
+    lib.sdlm_kv_gather_batch.restype = C.c_int
+    lib.sdlm_kv_gather_batch.argtypes = [vp, i32, i32, vp, vp, vp, vp]
+    lib.sdlm_sample.restype = C.c_int
+    lib.sdlm_sample.argtypes = [vp, i32, i32, C.c_int, vp, i64] + [vp] * 10
     lib.sdlm_verify_commit.restype = C.c_int
     lib.sdlm_verify_commit.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.sdlm_accept_commit.restype = C.c_int
@@ -210,6 +272,21 @@ def _host(t: torch.Tensor, dtype, name: str) -> torch.Tensor:
     if not (isinstance(t, torch.Tensor) and not t.is_cuda and t.dtype == dtype and t.is_contiguous()):
         raise TypeError(f"{name}: expected a contiguous host tensor of {dtype}")
     return t
+
+
+def _row_stride(t: torch.Tensor, d: int, name: str) -> int:
+    """Elements between the rows of a [batch, D, heads, d] tensor whose rows are evenly spaced, heads contiguous."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 4 and int(t.shape[3]) == d):
+        raise TypeError(f"{name}: expected a CUDA tensor of torch.bfloat16, [batch, D, heads, {d}]")
+    batch, D, heads = (int(x) for x in t.shape[:3])
+    if t.stride(3) != 1 or (heads > 1 and t.stride(2) != d):
+        raise TypeError(f"{name}: the heads of a row have to be contiguous")
+    if D > 1:
+        stride = int(t.stride(1))
+        if batch > 1 and t.stride(0) != D * stride:
+            raise TypeError(f"{name}: the rows have to be evenly spaced")
+        return stride
+    return int(t.stride(0)) if batch > 1 else heads * d
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
@@ -608,6 +685,142 @@ class Sdlm:
         self._check("sdlm_swiglu", self.lib.sdlm_swiglu(self.ctx, rows, I, _ptr(gate_up),
                                                         _ptr(_dev(out, torch.bfloat16, "out")), _stream_ptr(stream)))
         return out
+
+    # ---- verification of a drafted tree, sampling ----------------------------------------
+    def qk_norm_rope(self, q: torch.Tensor, k: Optional[torch.Tensor], rope: RopeConfig,
+                     positions: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                     k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, relative: bool = False,
+                     q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                     seq_ids: Optional[torch.Tensor] = None, stream=None):
+        """sdlm_qk_norm_rope: q [batch, D, n_heads, d] and k [batch, D, n_heads2, d] or None; either may be a slice of
+        the heads of a wider tensor (a stacked q/k/v product)."""
+        d = self.cfg.head_dim
+        batch, D = int(q.shape[0]), int(q.shape[1])
+        q_stride, k_stride = _row_stride(q, d, "q"), 0
+        if k is not None:
+            if tuple(k.shape[:2]) != (batch, D):
+                raise ValueError("q and k must have the same rows")
+            k_stride = _row_stride(k, d, "k")
+        if positions is not None:
+            _dev(positions, torch.int32, "positions")
+            if positions.numel() != batch * D:
+                raise ValueError("positions must be [batch, D]")
+        for w, n in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if w is not None and _dev(w, torch.bfloat16, n).numel() != d:
+                raise ValueError(f"{n} must be [head_dim]")
+        if seq_ids is not None and _dev(seq_ids, torch.int32, "seq_ids").numel() != batch:
+            raise ValueError("seq_ids must be [batch]")
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
+        if k is not None and k_out is None:
+            k_out = torch.empty(k.shape, dtype=torch.bfloat16, device=self.device)
+        if _dev(q_out, torch.bfloat16, "q_out").shape != q.shape or (
+                k is not None and _dev(k_out, torch.bfloat16, "k_out").shape != k.shape):
+            raise ValueError("the outputs must have their inputs' shapes")
+        r = rope.to_c()
+        self._check("sdlm_qk_norm_rope", self.lib.sdlm_qk_norm_rope(
+            self.ctx, batch, D, _ptr(seq_ids), _ptr(positions), int(relative), C.byref(r), float(eps), int(q.shape[2]),
+            _ptr(q), q_stride, _ptr(q_weight), _ptr(q_out), 0 if k is None else int(k.shape[2]), _ptr(k), k_stride,
+            _ptr(k_weight), _ptr(k_out) if k is not None else None, _stream_ptr(stream)))
+        return q_out, k_out
+
+    def _check_tree(self, parent, n_nodes, seq_ids, q=None, k=None, v=None, out=None) -> None:
+        if parent.dim() != 2:
+            raise ValueError("parent must be [batch, n]")
+        batch, n = int(_dev(parent, torch.int32, "parent").shape[0]), int(parent.shape[1])
+        for t, name in ((n_nodes, "n_nodes"), (seq_ids, "seq_ids")):
+            if t is not None and _dev(t, torch.int32, name).numel() != batch:
+                raise ValueError(f"{name} must be [batch]")
+        for x, heads in ((q, self.cfg.n_q_heads), (out, self.cfg.n_q_heads), (k, self.cfg.n_kv_heads), (v, self.cfg.n_kv_heads)):
+            if x is not None and tuple(_dev(x[0], torch.bfloat16, x[1]).shape) != (batch, n, heads, self.cfg.head_dim):
+                raise ValueError(f"{x[1]} must be [batch, n, {heads}, {self.cfg.head_dim}]")
+
+    def tree_attn(self, q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor, parent: torch.Tensor,
+                  n_nodes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                  seq_ids: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """sdlm_tree_attn: q [batch, n, Hq, d], k_tree / v_tree [batch, n, Hkv, d], parent [batch, n] int32.  Rows of
+        `out` behind a sequence's nodes are left as they are (zero when `out` is made here)."""
+        if out is None:
+            out = torch.empty_like(q) if n_nodes is None and seq_ids is None else torch.zeros_like(q)
+        self._check_tree(parent, n_nodes, seq_ids, (q, "q"), (k_tree, "k_tree"), (v_tree, "v_tree"), (out, "out"))
+        self._check("sdlm_tree_attn", self.lib.sdlm_tree_attn(
+            self.ctx, int(parent.shape[0]), int(parent.shape[1]), _ptr(seq_ids), _ptr(n_nodes), _ptr(parent), _ptr(q),
+            _ptr(k_tree), _ptr(v_tree), _ptr(out), _stream_ptr(stream)))
+        return out
+
+    def _tree_outputs(self, parent, draft_token, next_token, accepted_len, out_tokens, path):
+        shape = tuple(parent.shape)
+        if accepted_len is None:
+            accepted_len = torch.empty(shape[0], dtype=torch.int32, device=self.device)
+        if out_tokens is None:
+            out_tokens = torch.empty(shape, dtype=torch.int32, device=self.device)
+        if path is None:
+            path = torch.empty(shape, dtype=torch.int32, device=self.device)
+        for t, n in ((draft_token, "draft_token"), (next_token, "next_token"), (out_tokens, "out_tokens"), (path, "path")):
+            if tuple(_dev(t, torch.int32, n).shape) != shape:
+                raise ValueError(f"{n} must be [batch, n]")
+        if _dev(accepted_len, torch.int32, "accepted_len").numel() != shape[0]:
+            raise ValueError("accepted_len must be [batch]")
+        return accepted_len, out_tokens, path
+
+    def tree_commit(self, draft_token: torch.Tensor, next_token: torch.Tensor, parent: torch.Tensor, k_tree: torch.Tensor,
+                    v_tree: torch.Tensor, n_nodes: Optional[torch.Tensor] = None,
+                    accepted_len: Optional[torch.Tensor] = None, out_tokens: Optional[torch.Tensor] = None,
+                    path: Optional[torch.Tensor] = None, seq_ids: Optional[torch.Tensor] = None, stream=None):
+        """sdlm_tree_commit: draft_token, next_token, parent [batch, n] int32; returns accepted_len, out_tokens, path."""
+        self._check_tree(parent, n_nodes, seq_ids, k=(k_tree, "k_tree"), v=(v_tree, "v_tree"))
+        accepted_len, out_tokens, path = self._tree_outputs(parent, draft_token, next_token, accepted_len, out_tokens, path)
+        self._check("sdlm_tree_commit", self.lib.sdlm_tree_commit(
+            self.ctx, int(parent.shape[0]), int(parent.shape[1]), _ptr(seq_ids), _ptr(n_nodes), _ptr(parent),
+            _ptr(draft_token), _ptr(next_token), _ptr(k_tree), _ptr(v_tree), _ptr(accepted_len), _ptr(out_tokens),
+            _ptr(path), _stream_ptr(stream)))
+        return accepted_len, out_tokens, path
+
+    def kv_gather_batch(self, k_out: torch.Tensor, v_out: torch.Tensor, seq_ids: Optional[torch.Tensor] = None,
+                        stream=None) -> None:
+        """sdlm_kv_gather_batch: k_out / v_out [batch, length, Hkv, d]; rows beyond a slot's length stay as they are."""
+        shape = (self.cfg.n_kv_heads, self.cfg.head_dim)
+        if k_out.dim() != 4 or tuple(k_out.shape[2:]) != shape or k_out.shape != v_out.shape:
+            raise ValueError("k_out and v_out must be [batch, length, Hkv, d]")
+        if seq_ids is not None and _dev(seq_ids, torch.int32, "seq_ids").numel() != int(k_out.shape[0]):
+            raise ValueError("seq_ids must be [batch]")
+        self._check("sdlm_kv_gather_batch", self.lib.sdlm_kv_gather_batch(
+            self.ctx, int(k_out.shape[0]), int(k_out.shape[1]), _ptr(seq_ids), _ptr(_dev(k_out, torch.bfloat16, "k_out")),
+            _ptr(_dev(v_out, torch.bfloat16, "v_out")), _stream_ptr(stream)))
+
+    def sample(self, logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+               top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+               min_p: Optional[torch.Tensor] = None, token: Optional[torch.Tensor] = None,
+               prob: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+               n_kept: Optional[torch.Tensor] = None, stream=None):
+        """sdlm_sample: logits [..., vocab] bf16 or float32 (rows may be strided), u and the filters one value a row;
+        returns token, prob, entropy, n_kept of the rows' shape."""
+        if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dtype in (torch.bfloat16, torch.float32)):
+            raise TypeError("logits: expected a CUDA tensor of torch.bfloat16 or torch.float32")
+        shape, V = tuple(logits.shape[:-1]), int(logits.shape[-1])
+        rows = logits.numel() // V if V else 0
+        if V > 1 and logits.stride(-1) != 1:
+            raise TypeError("logits: the vocabulary has to be contiguous")
+        if logits.dim() == 2 and rows > 1:
+            stride = int(logits.stride(0))
+        else:
+            stride = V
+            if not logits.is_contiguous():
+                raise TypeError("logits: only [rows, vocab] may have strided rows")
+        for t, dt, n in ((u, torch.float32, "u"), (temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
+                         (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
+            if t is not None and _dev(t, dt, n).numel() != rows:
+                raise ValueError(f"{n} must hold one value a row")
+        outs = []
+        for t, dt, n in ((token, torch.int32, "token"), (prob, torch.float32, "prob"), (entropy, torch.float32, "entropy"),
+                         (n_kept, torch.int32, "n_kept")):
+            outs.append(torch.empty(shape, dtype=dt, device=self.device) if t is None else t)
+            if _dev(outs[-1], dt, n).numel() != rows:
+                raise ValueError(f"{n} must hold one value a row")
+        self._check("sdlm_sample", self.lib.sdlm_sample(
+            self.ctx, rows, V, LOGITS_BF16 if logits.dtype == torch.bfloat16 else LOGITS_F32, _ptr(logits), stride, _ptr(u),
+            _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), *[_ptr(t) for t in outs], _stream_ptr(stream)))
+        return tuple(outs)
 
     def lmhead_confidence_static(self, hidden: torch.Tensor, w_lm: torch.Tensor, token: torch.Tensor,
                                  p_top1: torch.Tensor, entropy: torch.Tensor, max_logit: Optional[torch.Tensor] = None,

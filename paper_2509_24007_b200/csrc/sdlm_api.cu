@@ -43,6 +43,11 @@ WorkspaceLayout workspace_layout(const sdlm_config& c) {
   L.attn_max_items = kAttnMaxCtas + c.max_batch * c.n_kv_heads;
   L.attn_ml = take((size_t)L.attn_max_items * L.q_rows_pad * 2 * 4);
   L.attn_o = take((size_t)L.attn_max_items * L.q_rows_pad * c.head_dim * 4);
+  const size_t tree_rows = 2 * (size_t)kAttnMaxCtas * 256;  // two cut pieces of 256 stacked rows per thread block
+  L.tree_ml = take(tree_rows * 2 * 4);
+  L.tree_o = take(tree_rows * c.head_dim * 4);
+  L.tree_cuts = take(kAttnMaxCtas * sizeof(TreeCut));
+  L.tree_cnt = take((size_t)c.max_batch * 4);
   L.attn_cnt = take((size_t)c.max_batch * c.n_kv_heads * 12);  // per pair: a record for the merge kernel, an arrival count
   L.st_q = take(rows * c.n_q_heads * c.head_dim * 2);
   L.st_k = take(rows * c.n_kv_heads * c.head_dim * 2);
@@ -204,6 +209,10 @@ struct CommitParams {
   const int32_t* carry_len;
   int32_t* next_carry_len;  // null, or [batch]: min(gamma - 1, c_max), 0 for a row that failed; may be carry_len itself
   int c_max;
+  // Tree mode (path != null): k_blk / v_blk hold D rows per sequence, one for each node of its tree; rows path[b][0 ..
+  // path_len[b]) are appended (path_len -1: the sequence is refused), and out_tokens are the tokens those nodes decided on.
+  const int32_t* path_len;
+  const int32_t* path;
   float tau, inv_ln_vocab;
   int mode, batch, D, Hkv, d, mpps, num_pages;
 };
@@ -256,8 +265,14 @@ __device__ __forceinline__ void accept_commit_body(const CommitParams& p, bool w
     int g = 0, na = 0, need = 0, state = 0, len = 0;
     if (i < p.batch) {
       const int slot = p.seq_ids ? p.seq_ids[i] : i;
-      len = *(volatile int32_t*)&p.seq_len[slot];
-      g = gamma_tau(p, i);
+      if (p.path) {
+        g = p.path_len[i];  // -1: a slot number that must not be followed
+        if (g < 0) { state = 1; g = 0; }
+        else len = *(volatile int32_t*)&p.seq_len[slot];
+      } else {
+        len = *(volatile int32_t*)&p.seq_len[slot];
+        g = gamma_tau(p, i);
+      }
       na = g;
       if (p.carry_len) {
         const int c = p.carry_len[i];
@@ -265,7 +280,7 @@ __device__ __forceinline__ void accept_commit_body(const CommitParams& p, bool w
         na = min(max(c, 0), p.c_max) + 1;
       }
       if (len + na > p.mpps * kPageSize) state = 1;
-      if (state == 0) need = (len % kPageSize == 0) || (len % kPageSize + na > kPageSize);
+      if (state == 0 && na > 0) need = (len % kPageSize == 0) || (len % kPageSize + na > kPageSize);
     }
     // exclusive scan of `need` in batch order
     int incl = need;
@@ -322,7 +337,7 @@ __device__ __forceinline__ void accept_commit_body(const CommitParams& p, bool w
     }
     if (tid == 0 && write_outputs) p.accepted_len[b] = g;
     for (int k = tid; write_outputs && k < p.D; k += kCommitThreads)
-      p.out_tokens[b * p.D + k] = (k < g) ? p.token[b * p.D + k] : -1;
+      p.out_tokens[b * p.D + k] = (k < g) ? p.token[b * p.D + (p.path ? p.path[b * p.D + k] : k)] : -1;
     if (need) {  // a page fresh from the ring may hold anything: clear its V^T tiles first
       const int per_head = kPageSize * p.d / 8;
       for (int idx = tid; idx < p.Hkv * per_head; idx += kCommitThreads)
@@ -341,7 +356,8 @@ __device__ __forceinline__ void accept_commit_body(const CommitParams& p, bool w
       const int pos = len + t;
       const int pidx = pos / kPageSize, key = pos % kPageSize;
       const int page = (need && pidx == new_idx) ? new_page : p.page_table[(size_t)slot * p.mpps + pidx];
-      const int srow = p.carry_len ? (t < na - 1 ? t : p.c_max) : t;  // carry rows, then the block's position 0
+      // carry rows, then the block's position 0; or the nodes of the accepted path
+      const int srow = p.path ? p.path[b * p.D + t] : p.carry_len ? (t < na - 1 ? t : p.c_max) : t;
       const size_t src = (((size_t)b * rows_per_seq + srow) * p.Hkv + h) * p.d;
       *reinterpret_cast<uint4*>(p.pool + kv_tile_offset(page, h, 0, p.Hkv, p.d) + k_tile_elem(key, c * 8)) =
           *(reinterpret_cast<const uint4*>(p.k_blk + src) + c);
@@ -397,6 +413,96 @@ __global__ void __launch_bounds__(kCommitThreads) accept_commit_layers_kernel(Co
   p.hdr = l.hdr; p.page_table = l.page_table; p.seq_len = l.seq_len; p.free_list = l.free_list;
   p.pool = l.pool; p.k_blk = l.k_blk; p.v_blk = l.v_blk;
   accept_commit_body(p, blockIdx.y == 0);
+}
+
+// The accepted path of a drafted tree, one warp a sequence: from node 0 to the lowest-numbered child whose draft token is
+// the one the verification pass decided on at its parent, and so on.  Lane i holds nodes i and i + 32; each step is
+// one shuffle and two votes.  Writes the path (-1 behind its end) and its length for the commit kernel.
+__global__ void __launch_bounds__(128) tree_walk_kernel(const int32_t* draft, const int32_t* next, const int32_t* parent,
+                                                        const int32_t* n_nodes, const int32_t* seq_ids, int32_t* path_len,
+                                                        int32_t* path, int batch, int n, int max_batch) {
+  ptx::grid_dep_launch();
+  ptx::grid_dep_wait();
+  const int b = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (b >= batch) return;
+  const int nodes = n_nodes ? min(max(n_nodes[b], 0), n) : n;
+  int up[2], tok[2], nx[2], way[2] = {-1, -1};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int node = lane + 32 * i;
+    const bool have = node < nodes;
+    up[i] = have ? parent[(size_t)b * n + node] : -1;
+    tok[i] = have ? draft[(size_t)b * n + node] : 0;
+    nx[i] = have ? next[(size_t)b * n + node] : 0;
+    if (up[i] >= node) up[i] = -1;  // not an earlier node: hangs from the history
+  }
+  // a slot number outside the tables, or one that another sequence of the call has too, must not be written to
+  bool bad = false;
+  if (seq_ids) {
+    const int slot = seq_ids[b];
+    bad = slot < 0 || slot >= max_batch;
+    for (int i = lane; i < batch; i += 32) bad |= i != b && seq_ids[i] == slot;
+  } else {
+    bad = b >= max_batch;
+  }
+  bad = __any_sync(0xffffffffu, bad);
+  int len = 0;
+  if (nodes > 0) {
+    int cur = 0;
+    while (cur >= 0) {  // cur grows with every step
+      if (lane == (len & 31)) way[len >> 5] = cur;
+      ++len;
+      const int a = __shfl_sync(0xffffffffu, nx[0], cur & 31), c = __shfl_sync(0xffffffffu, nx[1], cur & 31);
+      const int want = cur < 32 ? a : c;
+      const uint32_t m0 = __ballot_sync(0xffffffffu, lane < nodes && up[0] == cur && tok[0] == want);
+      const uint32_t m1 = __ballot_sync(0xffffffffu, lane + 32 < nodes && up[1] == cur && tok[1] == want);
+      cur = m0 ? __ffs(m0) - 1 : m1 ? 31 + __ffs(m1) : -1;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (lane + 32 * i < n) path[(size_t)b * n + lane + 32 * i] = bad ? -1 : way[i];
+  if (lane == 0) path_len[b] = bad ? -1 : len;
+}
+
+// Logical contents of several slots at once, [batch, length, Hkv, d]: a thread block takes one page of one KV head,
+// reads it in the pool's layout (V^T turned through shared memory) and writes whole rows.
+__global__ void __launch_bounds__(256) kv_gather_batch_kernel(const __nv_bfloat16* pool, const int32_t* page_table,
+                                                              const int32_t* seq_len, const int32_t* seq_ids, DevHeader* hdr,
+                                                              __nv_bfloat16* k_out, __nv_bfloat16* v_out, int length, int mpps,
+                                                              int max_batch, int num_pages, int Hkv, int d) {
+  __shared__ __align__(16) __nv_bfloat16 vt[kPageSize * 128];
+  ptx::grid_dep_launch();
+  ptx::grid_dep_wait();
+  const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, cpr = d / 8;
+  const int slot = seq_ids ? seq_ids[b] : b;
+  if (slot < 0 || slot >= max_batch) {
+    if (tid == 0) report_status(hdr, SDLM_ERR_DEVICE_CHECK, slot, b);
+    return;
+  }
+  const int have = min(min(seq_len[slot], length), mpps * kPageSize);
+  for (int pg = blockIdx.x; pg * kPageSize < have; pg += gridDim.x) {
+    const int page = page_table[(size_t)slot * mpps + pg], rows = min(kPageSize, have - pg * kPageSize);
+    if (page < 0 || page >= num_pages) {
+      if (tid == 0) report_status(hdr, SDLM_ERR_DEVICE_CHECK, slot, page);
+      continue;
+    }
+    const __nv_bfloat16* k_tile = pool + kv_tile_offset(page, h, 0, Hkv, d);
+    const uint4* v_tile = reinterpret_cast<const uint4*>(k_tile + kv_tile_elems(d));
+    for (int i = tid; i < kPageSize * cpr; i += 256) reinterpret_cast<uint4*>(vt)[i] = v_tile[i];
+    __syncthreads();
+    for (int i = tid; i < rows * cpr; i += 256) {
+      const int key = i / cpr, c = i % cpr;
+      const size_t dst = (((size_t)b * length + pg * kPageSize + key) * Hkv + h) * d + c * 8;
+      *reinterpret_cast<uint4*>(k_out + dst) = *reinterpret_cast<const uint4*>(k_tile + k_tile_elem(key, c * 8));
+      uint4 vv;
+      __nv_bfloat16* ve = reinterpret_cast<__nv_bfloat16*>(&vv);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ve[e] = vt[vt_tile_elem(key, c * 8 + e)];
+      *reinterpret_cast<uint4*>(v_out + dst) = vv;
+    }
+    __syncthreads();
+  }
 }
 
 }  // namespace sdlm
@@ -544,7 +650,8 @@ extern "C" sdlm_status sdlm_create(const sdlm_config* cfg, void* kv_pool, size_t
   ctx->defer_merge = 0;
   ctx->pending_merge_fn = nullptr;
   ctx->tmap_h_rows = ctx->tmap_h_box = 0;
-  if (setup_attn(ctx) != cudaSuccess || setup_causal(ctx) != cudaSuccess || setup_lmhead(ctx) != cudaSuccess) { delete ctx; return SDLM_ERR_CUDA; }
+  if (setup_attn(ctx) != cudaSuccess || setup_causal(ctx) != cudaSuccess || setup_lmhead(ctx) != cudaSuccess ||
+      setup_tree(ctx) != cudaSuccess || setup_sample(ctx) != cudaSuccess) { delete ctx; return SDLM_ERR_CUDA; }
   sdlm_status s = reset_tables(ctx, nullptr, 0);
   if (s == SDLM_OK && cudaStreamSynchronize(0) != cudaSuccess) s = SDLM_ERR_CUDA;
   if (s != SDLM_OK) { delete ctx; return s; }
@@ -758,6 +865,7 @@ static sdlm_status accept_commit_launch(sdlm_ctx* ctx, int32_t batch, int32_t D,
   p.carry_len = carry_len;
   p.next_carry_len = next_carry_len;
   p.c_max = c_max;
+  p.path_len = nullptr; p.path = nullptr;
   p.tau = tau;
   p.inv_ln_vocab = c.vocab > 1 ? (float)(1.0 / log((double)c.vocab)) : 0.0f;
   p.mode = (int)mode; p.batch = batch; p.D = D; p.Hkv = c.n_kv_heads; p.d = c.head_dim;
@@ -1188,4 +1296,88 @@ extern "C" sdlm_status sdlm_decode_step_host(sdlm_ctx* ctx, int32_t batch, int32
     ok &= cudaMemcpyAsync(out_tokens_host, d_out_tokens, rows * 4, cudaMemcpyDeviceToHost, st) == cudaSuccess;
   if (!ok || cudaStreamSynchronize(st) != cudaSuccess) return SDLM_ERR_CUDA;
   return SDLM_OK;
+}
+
+// Walks the trees, then one launch commits the accepted paths into every cache.
+static sdlm_status tree_commit_launch(sdlm_ctx* const* ctxs, int32_t n_layers, int32_t batch, int32_t n,
+                                      const int32_t* seq_ids, const int32_t* n_nodes, const int32_t* parent,
+                                      const int32_t* draft_token, const int32_t* next_token, const void* const* k_tree,
+                                      const void* const* v_tree, int32_t* accepted_len, int32_t* out_tokens, int32_t* path,
+                                      void* stream) {
+  if (!ctxs || n_layers < 1 || !parent || !draft_token || !next_token || !k_tree || !v_tree || !accepted_len || !out_tokens || !path)
+    return SDLM_ERR_INVALID_ARG;
+  if (batch < 1 || n < 1) return SDLM_ERR_INVALID_ARG;
+  if (n_layers > kMaxCommitLayers || n > kMaxTreeNodes) return SDLM_ERR_SHAPE;
+  sdlm_ctx* c0 = ctxs[0];
+  if (!c0) return SDLM_ERR_INVALID_ARG;
+  if (batch > c0->cfg.max_batch) return SDLM_ERR_SHAPE;
+  CommitLayers* L = new (std::nothrow) CommitLayers;
+  if (!L) return SDLM_ERR_CUDA;
+  for (int l = 0; l < n_layers; ++l) {
+    sdlm_ctx* c = ctxs[l];
+    bool ok = c && k_tree[l] && v_tree[l] && aligned16(k_tree[l]) && aligned16(v_tree[l]) && same_device(c) &&
+              memcmp(&c->cfg, &c0->cfg, sizeof(sdlm_config)) == 0;
+    for (int i = 0; ok && i < l; ++i) ok = ctxs[i] != c;  // two commits into one cache would write the same rows
+    if (!ok) {
+      delete L;
+      return SDLM_ERR_INVALID_ARG;
+    }
+    L->layer[l] = CommitLayer{c->hdr, c->page_table, c->seq_len, c->free_list, reinterpret_cast<__nv_bfloat16*>(c->pool),
+                              static_cast<const __nv_bfloat16*>(k_tree[l]), static_cast<const __nv_bfloat16*>(v_tree[l])};
+  }
+  const sdlm_config& c = c0->cfg;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int32_t* path_len = reinterpret_cast<int32_t*>(c0->ws + c0->lay.tree_cnt);
+  cudaError_t e = launch_overlapped(tree_walk_kernel, dim3((batch + 3) / 4), dim3(128), 0, st, draft_token, next_token, parent,
+                                    n_nodes, seq_ids, path_len, path, batch, n, c.max_batch);
+  c0->launches++;
+  if (e == cudaSuccess) {
+    CommitParams p{};
+    p.seq_ids = seq_ids; p.token = next_token;
+    p.accepted_len = accepted_len; p.out_tokens = out_tokens;
+    p.path_len = path_len; p.path = path;
+    p.batch = batch; p.D = n; p.Hkv = c.n_kv_heads; p.d = c.head_dim;
+    p.mpps = c.max_pages_per_seq; p.num_pages = c.num_pages;
+    e = launch_overlapped(accept_commit_layers_kernel, dim3(batch, n_layers), dim3(kCommitThreads), 0, st, p, *L);
+    c0->launches++;
+  }
+  delete L;
+  return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? SDLM_OK : SDLM_ERR_CUDA;
+}
+
+extern "C" sdlm_status sdlm_tree_commit(sdlm_ctx* ctx, int32_t batch, int32_t n, const int32_t* seq_ids,
+                                        const int32_t* n_nodes, const int32_t* parent, const int32_t* draft_token,
+                                        const int32_t* next_token, const void* k_tree, const void* v_tree,
+                                        int32_t* accepted_len, int32_t* out_tokens, int32_t* path, void* stream) {
+  return tree_commit_launch(&ctx, 1, batch, n, seq_ids, n_nodes, parent, draft_token, next_token, &k_tree, &v_tree,
+                            accepted_len, out_tokens, path, stream);
+}
+
+extern "C" sdlm_status sdlm_tree_commit_layers(sdlm_ctx* const* ctxs, int32_t n_layers, int32_t batch, int32_t n,
+                                               const int32_t* seq_ids, const int32_t* n_nodes, const int32_t* parent,
+                                               const int32_t* draft_token, const int32_t* next_token,
+                                               const void* const* k_tree, const void* const* v_tree,
+                                               int32_t* accepted_len, int32_t* out_tokens, int32_t* path, void* stream) {
+  return tree_commit_launch(ctxs, n_layers, batch, n, seq_ids, n_nodes, parent, draft_token, next_token, k_tree, v_tree,
+                            accepted_len, out_tokens, path, stream);
+}
+
+extern "C" sdlm_status sdlm_kv_gather_batch(sdlm_ctx* ctx, int32_t batch, int32_t length, const int32_t* seq_ids, void* k_out,
+                                            void* v_out, void* stream) {
+  if (!ctx || batch < 1 || length < 0) return SDLM_ERR_INVALID_ARG;
+  if (batch > ctx->cfg.max_batch) return SDLM_ERR_SHAPE;
+  if (length == 0) return SDLM_OK;
+  if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out)) return SDLM_ERR_INVALID_ARG;
+  if (!same_device(ctx)) return SDLM_ERR_INVALID_ARG;
+  const sdlm_config& c = ctx->cfg;
+  if (c.n_kv_heads > 65535) return SDLM_ERR_UNSUPPORTED;
+  const long long most = length < (long long)c.max_pages_per_seq * kPageSize ? length : (long long)c.max_pages_per_seq * kPageSize;
+  const int pages = (int)((most + kPageSize - 1) / kPageSize);
+  const cudaError_t e = launch_overlapped(kv_gather_batch_kernel, dim3(pages < 4096 ? pages : 4096, c.n_kv_heads, batch), dim3(256),
+                                          0, static_cast<cudaStream_t>(stream), reinterpret_cast<const __nv_bfloat16*>(ctx->pool),
+                                          ctx->page_table, ctx->seq_len, seq_ids, ctx->hdr, static_cast<__nv_bfloat16*>(k_out),
+                                          static_cast<__nv_bfloat16*>(v_out), length, c.max_pages_per_seq, c.max_batch,
+                                          c.num_pages, c.n_kv_heads, c.head_dim);
+  ctx->launches++;
+  return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? SDLM_OK : SDLM_ERR_CUDA;
 }

@@ -15,6 +15,7 @@ constexpr int kMaxBlock = 8;         // largest D
 constexpr int kMaxBlockKeys = 16;    // rows of k_blk / v_blk per sequence in the masked variant
 constexpr int kMaxQRows = 64;        // (Hq/Hkv) * D stacked query rows per KV head
 constexpr int kMaxBatch = 4096;
+constexpr int kMaxTreeNodes = 64;    // nodes of a drafted tree: one key tile, one visibility word
 constexpr int kLinSplitMax = 12;      // most K ranges of a split-K linear
 constexpr int kLinSplitMaxN = 4096;   // widest output that may be cut into kLinSplitMax K ranges (sizes the partial sums)
 constexpr int kLinSplitWideN = 8192;  // widest output a split-K linear takes: fewer ranges, the same partial-sum buffer
@@ -38,11 +39,19 @@ struct WorkspaceLayout {
   size_t lin_part;                                         // float [kLinSplitMax][128][kLinSplitMaxN]
   size_t lm_partials;                                      // float4 [kLmMaxStripes][max_rows]
   size_t attn_ml, attn_o;                                  // split-KV partial (m, l) and O
+  size_t tree_ml, tree_o, tree_cuts;                       // tree attention: partial results and where they are cut
+  size_t tree_cnt;                                         // accepted path length per sequence (tree commit)
   size_t attn_cnt;                                         // per (batch row, KV head): record for the merge kernel, arrival count
   size_t st_q, st_k, st_v, st_hidden, st_out, st_seq_ids, st_token, st_p, st_ent, st_acc, st_out_tokens;
   size_t total;
   int attn_max_items;
   int q_rows_pad;  // stacked query rows per KV head at max_block, padded to 32 or 64
+};
+
+// The task of tree attention that holds the first position of a thread block's range (see sdlm_tree.cu).
+struct TreeCut {
+  long long start, span, total;  // the task's first position, positions per thread block (0: no work), positions in all
+  int b, hk, rt, groups, nodes;
 };
 
 bool config_valid(const sdlm_config& c);
@@ -157,6 +166,12 @@ inline cudaError_t launch_overlapped_cluster(void (*kernel)(KArgs...), dim3 grid
   return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
 }
 
+// Whether the context's device is the current one: its memory and its streams are that device's.
+inline bool same_device(const sdlm_ctx* ctx) {
+  int dev = -1;
+  return cudaGetDevice(&dev) == cudaSuccess && dev == ctx->device;
+}
+
 // ---- launchers implemented in the kernel translation units ---------------------------------
 // Visibility of the block's own keys built inside the kernel (kind 1: verification inputs, 2: carry rows in
 // front of the block), and which of the q_stride positions per sequence one launch computes.
@@ -216,6 +231,8 @@ cudaError_t launch_rmsnorm(sdlm_ctx* ctx, int rows, int H, const void* x, const 
 cudaError_t launch_pending_merge(sdlm_ctx* ctx, cudaStream_t st);
 cudaError_t launch_causal_attn(sdlm_ctx* ctx, int slot, int first_pos, int n_rows, const void* q, void* out, cudaStream_t st);
 cudaError_t setup_causal(sdlm_ctx* ctx);
+cudaError_t setup_tree(sdlm_ctx* ctx);
+cudaError_t setup_sample(sdlm_ctx* ctx);
 cudaError_t setup_attn(sdlm_ctx* ctx);
 cudaError_t setup_lmhead(sdlm_ctx* ctx);
 
