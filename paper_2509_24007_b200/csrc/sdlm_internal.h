@@ -50,8 +50,8 @@ struct WorkspaceLayout {
 
 // The task of tree attention that holds the first position of a thread block's range (see sdlm_tree.cu).
 struct TreeCut {
-  long long start, span, total;  // the task's first position, positions per thread block (0: no work), positions in all
-  int b, hk, rt, groups, nodes;
+  int start, span, total;  // the task's first position, positions per thread block (0: no work), positions in all
+  int b, hk, rt, tiles, nodes;
 };
 
 bool config_valid(const sdlm_config& c);

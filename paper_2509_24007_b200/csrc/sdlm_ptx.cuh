@@ -111,6 +111,33 @@ __device__ __forceinline__ bool mbar_wait_parked(uint64_t* bar, uint32_t parity,
     }
   }
 }
+// Waits of a whole warp on a pipeline's critical path; every lane gets the outcome.  A poll takes some 100 cycles even
+// when the phase is complete and the vote on it 50 more, so two barriers are polled at once (bar_b may be null); reading
+// the clock takes 600, so it is looked at only after the first polls have failed.  The same bound and abort rule.
+__device__ __forceinline__ bool mbar_wait2_warp(uint64_t* bar_a, uint32_t parity_a, uint64_t* bar_b, uint32_t parity_b,
+                                                volatile int* abort) {
+  uint64_t t0 = 0;
+  for (uint32_t i = 0;; ++i) {
+    const bool a = i == 0 ? mbar_try_wait(bar_a, parity_a) : mbar_try_wait_parked(bar_a, parity_a, 20000u);
+    const bool b = !bar_b || (i == 0 ? mbar_try_wait(bar_b, parity_b) : mbar_try_wait_parked(bar_b, parity_b, 20000u));
+    if (__all_sync(0xffffffffu, a && b)) return true;
+    if ((i & 15u) == 15u) {
+      bool out = *abort != 0;
+      if (!out) {
+        const uint64_t now = global_ns();
+        if (t0 == 0) t0 = now;
+        out = now - t0 > kWaitLimitNs;
+      }
+      if (__any_sync(0xffffffffu, out)) {
+        *abort = 1;
+        return false;
+      }
+    }
+  }
+}
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  return mbar_wait2_warp(bar, parity, nullptr, 0, abort);
+}
 // The same for a whole warp whose wait is long and whose wake-up need not be prompt (a warp that takes an
 // item's results at the item's end, a stage that is refilled a group later): only lane 0 polls, with a
 // pause between polls, so that the waiting warp leaves the issue slots of its scheduler to the warps that
