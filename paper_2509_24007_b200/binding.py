@@ -68,17 +68,14 @@ def tree_commit_layers(contexts, draft_token, next_token, parent, k_trees, v_tre
     n_layers = len(contexts)
     if len(k_trees) != n_layers or len(v_trees) != n_layers:
         raise ValueError("k_trees and v_trees must hold one tensor per context")
-    for k, v in zip(k_trees, v_trees):
-        sd0._check_tree(parent, n_nodes, seq_ids, k=(k, "k_tree"), v=(v, "v_tree"))
-    accepted_len, out_tokens, path = sd0._tree_outputs(parent, draft_token, next_token, accepted_len, out_tokens, path)
+    before, after, outs = sd0._tree_commit_args(parent, n_nodes, seq_ids, draft_token, next_token, accepted_len, out_tokens, path)
+    rows = (*parent.shape, sd0.cfg.n_kv_heads, sd0.cfg.head_dim)
     ctx_arr = (C.c_void_p * n_layers)(*[c.ctx.value for c in contexts])
-    k_arr = (C.c_void_p * n_layers)(*[_ptr(t) for t in k_trees])
-    v_arr = (C.c_void_p * n_layers)(*[_ptr(t) for t in v_trees])
+    k_arr = (C.c_void_p * n_layers)(*[_shaped(t, torch.bfloat16, rows, "k_tree") for t in k_trees])
+    v_arr = (C.c_void_p * n_layers)(*[_shaped(t, torch.bfloat16, rows, "v_tree") for t in v_trees])
     sd0._check("sdlm_tree_commit_layers", sd0.lib.sdlm_tree_commit_layers(
-        ctx_arr, n_layers, int(parent.shape[0]), int(parent.shape[1]), _ptr(seq_ids), _ptr(n_nodes), _ptr(parent),
-        _ptr(draft_token), _ptr(next_token), k_arr, v_arr, _ptr(accepted_len), _ptr(out_tokens), _ptr(path),
-        _stream_ptr(stream)))
-    return accepted_len, out_tokens, path
+        ctx_arr, n_layers, *parent.shape, *before, k_arr, v_arr, *after, _stream_ptr(stream)))
+    return outs
 
 
 class SdlmError(RuntimeError):
@@ -126,6 +123,13 @@ class RopeConfig:
     attn_factor: float = 0.0
 
     def to_c(self) -> _Rope:
+        key = (self.theta, self.rot_dim, self.interleaved, self.scaling, self.factor, self.trained_len, self.beta_fast,
+               self.beta_slow, self.attn_factor)
+        if getattr(self, "_c_of", None) != key:  # made again only when a field has changed
+            self._c_of, self._c = key, self._struct()
+        return self._c
+
+    def _struct(self) -> _Rope:
         return _Rope(self.theta, self.rot_dim, int(self.interleaved), int(self.scaling), self.factor, self.trained_len,
                      self.beta_fast, self.beta_slow, self.attn_factor)
 
@@ -276,21 +280,47 @@ def _host(t: torch.Tensor, dtype, name: str) -> torch.Tensor:
 
 def _row_stride(t: torch.Tensor, d: int, name: str) -> int:
     """Elements between the rows of a [batch, D, heads, d] tensor whose rows are evenly spaced, heads contiguous."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 4 and int(t.shape[3]) == d):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.bfloat16 and t.dim() == 4 and t.shape[3] == d):
         raise TypeError(f"{name}: expected a CUDA tensor of torch.bfloat16, [batch, D, heads, {d}]")
-    batch, D, heads = (int(x) for x in t.shape[:3])
-    if t.stride(3) != 1 or (heads > 1 and t.stride(2) != d):
+    batch, D, heads, _ = t.shape
+    st = t.stride()
+    if st[3] != 1 or (heads > 1 and st[2] != d):
         raise TypeError(f"{name}: the heads of a row have to be contiguous")
     if D > 1:
-        stride = int(t.stride(1))
-        if batch > 1 and t.stride(0) != D * stride:
+        if batch > 1 and st[0] != D * st[1]:
             raise TypeError(f"{name}: the rows have to be evenly spaced")
-        return stride
-    return int(t.stride(0)) if batch > 1 else heads * d
+        return st[1]
+    return st[0] if batch > 1 else heads * d
+
+
+# torch's raw handle of the current stream, without a Stream object around it (2 us a call); by its public name otherwise
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
     return (stream or torch.cuda.current_stream()).cuda_stream
+
+
+def _is(t, dtype, numel: int, name: str) -> int:
+    """Address of a contiguous CUDA tensor of `numel` elements of dtype; None stays None."""
+    if t is None:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.is_contiguous()):
+        raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}")
+    if t.numel() != numel:
+        raise ValueError(f"{name}: expected {numel} elements")
+    return t.data_ptr()
+
+
+def _shaped(t, dtype, shape, name: str) -> int:
+    """Address of a contiguous CUDA tensor of that shape."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.is_contiguous()):
+        raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected the shape {tuple(shape)}")
+    return t.data_ptr()
 
 
 class Sdlm:
@@ -419,7 +449,11 @@ class Sdlm:
         return dev_buf
 
     def kv_restore(self, dev_buf: torch.Tensor, stream=None) -> None:
-        self.kv_pages(KV_RESTORE, dev_buf=dev_buf, stream=stream)
+        _dev(dev_buf, torch.uint8, "dev_buf")
+        a = _KvArgs(dev_buf=dev_buf.data_ptr(), dev_bytes=dev_buf.numel())
+        code = self.lib.sdlm_kv_pages(self.ctx, KV_RESTORE, C.byref(a), None, _stream_ptr(stream))
+        if code:
+            self._check("sdlm_kv_pages", code)
 
     def kv_import(self, buf: np.ndarray) -> None:
         self.kv_pages(KV_IMPORT, host_buf=np.ascontiguousarray(buf))
@@ -695,45 +729,34 @@ class Sdlm:
         """sdlm_qk_norm_rope: q [batch, D, n_heads, d] and k [batch, D, n_heads2, d] or None; either may be a slice of
         the heads of a wider tensor (a stacked q/k/v product)."""
         d = self.cfg.head_dim
-        batch, D = int(q.shape[0]), int(q.shape[1])
-        q_stride, k_stride = _row_stride(q, d, "q"), 0
-        if k is not None:
-            if tuple(k.shape[:2]) != (batch, D):
-                raise ValueError("q and k must have the same rows")
-            k_stride = _row_stride(k, d, "k")
-        if positions is not None:
-            _dev(positions, torch.int32, "positions")
-            if positions.numel() != batch * D:
-                raise ValueError("positions must be [batch, D]")
-        for w, n in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-            if w is not None and _dev(w, torch.bfloat16, n).numel() != d:
-                raise ValueError(f"{n} must be [head_dim]")
-        if seq_ids is not None and _dev(seq_ids, torch.int32, "seq_ids").numel() != batch:
-            raise ValueError("seq_ids must be [batch]")
+        q_stride = _row_stride(q, d, "q")
+        batch, D, heads, _ = q.shape
+        heads2 = k_stride = 0
+        k_ptr = k_out_ptr = None
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
-        if k is not None and k_out is None:
-            k_out = torch.empty(k.shape, dtype=torch.bfloat16, device=self.device)
-        if _dev(q_out, torch.bfloat16, "q_out").shape != q.shape or (
-                k is not None and _dev(k_out, torch.bfloat16, "k_out").shape != k.shape):
-            raise ValueError("the outputs must have their inputs' shapes")
-        r = rope.to_c()
-        self._check("sdlm_qk_norm_rope", self.lib.sdlm_qk_norm_rope(
-            self.ctx, batch, D, _ptr(seq_ids), _ptr(positions), int(relative), C.byref(r), float(eps), int(q.shape[2]),
-            _ptr(q), q_stride, _ptr(q_weight), _ptr(q_out), 0 if k is None else int(k.shape[2]), _ptr(k), k_stride,
-            _ptr(k_weight), _ptr(k_out) if k is not None else None, _stream_ptr(stream)))
+        if k is not None:
+            k_stride = _row_stride(k, d, "k")
+            if k.shape[0] != batch or k.shape[1] != D:
+                raise ValueError("q and k must have the same rows")
+            heads2, k_ptr = k.shape[2], k.data_ptr()
+            if k_out is None:
+                k_out = torch.empty(k.shape, dtype=torch.bfloat16, device=self.device)
+            k_out_ptr = _shaped(k_out, torch.bfloat16, k.shape, "k_out")
+        code = self.lib.sdlm_qk_norm_rope(
+            self.ctx, batch, D, _is(seq_ids, torch.int32, batch, "seq_ids"), _is(positions, torch.int32, batch * D, "positions"),
+            1 if relative else 0, C.byref(rope.to_c()), eps, heads, q.data_ptr(), q_stride,
+            _is(q_weight, torch.bfloat16, d, "q_weight"), _shaped(q_out, torch.bfloat16, q.shape, "q_out"), heads2, k_ptr, k_stride,
+            _is(k_weight, torch.bfloat16, d, "k_weight"), k_out_ptr, _stream_ptr(stream))
+        if code:
+            self._check("sdlm_qk_norm_rope", code)
         return q_out, k_out
 
-    def _check_tree(self, parent, n_nodes, seq_ids, q=None, k=None, v=None, out=None) -> None:
-        if parent.dim() != 2:
+    def _tree_shape(self, parent: torch.Tensor):
+        """(batch, n) of a tensor of parents."""
+        if not isinstance(parent, torch.Tensor) or parent.dim() != 2:
             raise ValueError("parent must be [batch, n]")
-        batch, n = int(_dev(parent, torch.int32, "parent").shape[0]), int(parent.shape[1])
-        for t, name in ((n_nodes, "n_nodes"), (seq_ids, "seq_ids")):
-            if t is not None and _dev(t, torch.int32, name).numel() != batch:
-                raise ValueError(f"{name} must be [batch]")
-        for x, heads in ((q, self.cfg.n_q_heads), (out, self.cfg.n_q_heads), (k, self.cfg.n_kv_heads), (v, self.cfg.n_kv_heads)):
-            if x is not None and tuple(_dev(x[0], torch.bfloat16, x[1]).shape) != (batch, n, heads, self.cfg.head_dim):
-                raise ValueError(f"{x[1]} must be [batch, n, {heads}, {self.cfg.head_dim}]")
+        return parent.shape
 
     def tree_attn(self, q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor, parent: torch.Tensor,
                   n_nodes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
@@ -742,51 +765,59 @@ class Sdlm:
         `out` behind a sequence's nodes are left as they are (zero when `out` is made here)."""
         if out is None:
             out = torch.empty_like(q) if n_nodes is None and seq_ids is None else torch.zeros_like(q)
-        self._check_tree(parent, n_nodes, seq_ids, (q, "q"), (k_tree, "k_tree"), (v_tree, "v_tree"), (out, "out"))
-        self._check("sdlm_tree_attn", self.lib.sdlm_tree_attn(
-            self.ctx, int(parent.shape[0]), int(parent.shape[1]), _ptr(seq_ids), _ptr(n_nodes), _ptr(parent), _ptr(q),
-            _ptr(k_tree), _ptr(v_tree), _ptr(out), _stream_ptr(stream)))
+        batch, n = self._tree_shape(parent)
+        c, bf16 = self.cfg, torch.bfloat16
+        rows, kv_rows = (batch, n, c.n_q_heads, c.head_dim), (batch, n, c.n_kv_heads, c.head_dim)
+        code = self.lib.sdlm_tree_attn(
+            self.ctx, batch, n, _is(seq_ids, torch.int32, batch, "seq_ids"), _is(n_nodes, torch.int32, batch, "n_nodes"),
+            _shaped(parent, torch.int32, (batch, n), "parent"), _shaped(q, bf16, rows, "q"),
+            _shaped(k_tree, bf16, kv_rows, "k_tree"), _shaped(v_tree, bf16, kv_rows, "v_tree"), _shaped(out, bf16, rows, "out"),
+            _stream_ptr(stream))
+        if code:
+            self._check("sdlm_tree_attn", code)
         return out
 
-    def _tree_outputs(self, parent, draft_token, next_token, accepted_len, out_tokens, path):
-        shape = tuple(parent.shape)
+    def _tree_commit_args(self, parent, n_nodes, seq_ids, draft_token, next_token, accepted_len, out_tokens, path):
+        """Checked outputs (made here where they are None) and the addresses in the order of the C call's arguments."""
+        batch, n = shape = self._tree_shape(parent)
+        i32 = torch.int32
         if accepted_len is None:
-            accepted_len = torch.empty(shape[0], dtype=torch.int32, device=self.device)
+            accepted_len = torch.empty(batch, dtype=i32, device=self.device)
         if out_tokens is None:
-            out_tokens = torch.empty(shape, dtype=torch.int32, device=self.device)
+            out_tokens = torch.empty(shape, dtype=i32, device=self.device)
         if path is None:
-            path = torch.empty(shape, dtype=torch.int32, device=self.device)
-        for t, n in ((draft_token, "draft_token"), (next_token, "next_token"), (out_tokens, "out_tokens"), (path, "path")):
-            if tuple(_dev(t, torch.int32, n).shape) != shape:
-                raise ValueError(f"{n} must be [batch, n]")
-        if _dev(accepted_len, torch.int32, "accepted_len").numel() != shape[0]:
-            raise ValueError("accepted_len must be [batch]")
-        return accepted_len, out_tokens, path
+            path = torch.empty(shape, dtype=i32, device=self.device)
+        before = [_is(seq_ids, i32, batch, "seq_ids"), _is(n_nodes, i32, batch, "n_nodes"), _shaped(parent, i32, shape, "parent"),
+                  _shaped(draft_token, i32, shape, "draft_token"), _shaped(next_token, i32, shape, "next_token")]
+        after = [_is(accepted_len, i32, batch, "accepted_len"), _shaped(out_tokens, i32, shape, "out_tokens"),
+                 _shaped(path, i32, shape, "path")]
+        return before, after, (accepted_len, out_tokens, path)
 
     def tree_commit(self, draft_token: torch.Tensor, next_token: torch.Tensor, parent: torch.Tensor, k_tree: torch.Tensor,
                     v_tree: torch.Tensor, n_nodes: Optional[torch.Tensor] = None,
                     accepted_len: Optional[torch.Tensor] = None, out_tokens: Optional[torch.Tensor] = None,
                     path: Optional[torch.Tensor] = None, seq_ids: Optional[torch.Tensor] = None, stream=None):
         """sdlm_tree_commit: draft_token, next_token, parent [batch, n] int32; returns accepted_len, out_tokens, path."""
-        self._check_tree(parent, n_nodes, seq_ids, k=(k_tree, "k_tree"), v=(v_tree, "v_tree"))
-        accepted_len, out_tokens, path = self._tree_outputs(parent, draft_token, next_token, accepted_len, out_tokens, path)
-        self._check("sdlm_tree_commit", self.lib.sdlm_tree_commit(
-            self.ctx, int(parent.shape[0]), int(parent.shape[1]), _ptr(seq_ids), _ptr(n_nodes), _ptr(parent),
-            _ptr(draft_token), _ptr(next_token), _ptr(k_tree), _ptr(v_tree), _ptr(accepted_len), _ptr(out_tokens),
-            _ptr(path), _stream_ptr(stream)))
-        return accepted_len, out_tokens, path
+        before, after, outs = self._tree_commit_args(parent, n_nodes, seq_ids, draft_token, next_token, accepted_len, out_tokens, path)
+        batch, n = parent.shape
+        rows = (batch, n, self.cfg.n_kv_heads, self.cfg.head_dim)
+        code = self.lib.sdlm_tree_commit(self.ctx, batch, n, *before, _shaped(k_tree, torch.bfloat16, rows, "k_tree"),
+                                         _shaped(v_tree, torch.bfloat16, rows, "v_tree"), *after, _stream_ptr(stream))
+        if code:
+            self._check("sdlm_tree_commit", code)
+        return outs
 
     def kv_gather_batch(self, k_out: torch.Tensor, v_out: torch.Tensor, seq_ids: Optional[torch.Tensor] = None,
                         stream=None) -> None:
         """sdlm_kv_gather_batch: k_out / v_out [batch, length, Hkv, d]; rows beyond a slot's length stay as they are."""
-        shape = (self.cfg.n_kv_heads, self.cfg.head_dim)
-        if k_out.dim() != 4 or tuple(k_out.shape[2:]) != shape or k_out.shape != v_out.shape:
+        if k_out.dim() != 4 or k_out.shape[2:] != (self.cfg.n_kv_heads, self.cfg.head_dim):
             raise ValueError("k_out and v_out must be [batch, length, Hkv, d]")
-        if seq_ids is not None and _dev(seq_ids, torch.int32, "seq_ids").numel() != int(k_out.shape[0]):
-            raise ValueError("seq_ids must be [batch]")
-        self._check("sdlm_kv_gather_batch", self.lib.sdlm_kv_gather_batch(
-            self.ctx, int(k_out.shape[0]), int(k_out.shape[1]), _ptr(seq_ids), _ptr(_dev(k_out, torch.bfloat16, "k_out")),
-            _ptr(_dev(v_out, torch.bfloat16, "v_out")), _stream_ptr(stream)))
+        batch, length = k_out.shape[:2]
+        code = self.lib.sdlm_kv_gather_batch(self.ctx, batch, length, _is(seq_ids, torch.int32, batch, "seq_ids"),
+                                             _shaped(k_out, torch.bfloat16, k_out.shape, "k_out"),
+                                             _shaped(v_out, torch.bfloat16, k_out.shape, "v_out"), _stream_ptr(stream))
+        if code:
+            self._check("sdlm_kv_gather_batch", code)
 
     def sample(self, logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None,
                top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
@@ -797,30 +828,26 @@ class Sdlm:
         returns token, prob, entropy, n_kept of the rows' shape."""
         if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dtype in (torch.bfloat16, torch.float32)):
             raise TypeError("logits: expected a CUDA tensor of torch.bfloat16 or torch.float32")
-        shape, V = tuple(logits.shape[:-1]), int(logits.shape[-1])
-        rows = logits.numel() // V if V else 0
-        if V > 1 and logits.stride(-1) != 1:
-            raise TypeError("logits: the vocabulary has to be contiguous")
-        if logits.dim() == 2 and rows > 1:
-            stride = int(logits.stride(0))
-        else:
-            stride = V
-            if not logits.is_contiguous():
-                raise TypeError("logits: only [rows, vocab] may have strided rows")
-        for t, dt, n in ((u, torch.float32, "u"), (temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
-                         (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
-            if t is not None and _dev(t, dt, n).numel() != rows:
-                raise ValueError(f"{n} must hold one value a row")
-        outs = []
-        for t, dt, n in ((token, torch.int32, "token"), (prob, torch.float32, "prob"), (entropy, torch.float32, "entropy"),
-                         (n_kept, torch.int32, "n_kept")):
-            outs.append(torch.empty(shape, dtype=dt, device=self.device) if t is None else t)
-            if _dev(outs[-1], dt, n).numel() != rows:
-                raise ValueError(f"{n} must hold one value a row")
-        self._check("sdlm_sample", self.lib.sdlm_sample(
-            self.ctx, rows, V, LOGITS_BF16 if logits.dtype == torch.bfloat16 else LOGITS_F32, _ptr(logits), stride, _ptr(u),
-            _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), *[_ptr(t) for t in outs], _stream_ptr(stream)))
-        return tuple(outs)
+        shape, V = logits.shape[:-1], logits.shape[-1]
+        rows, stride = logits.numel() // V if V else 0, V
+        if not logits.is_contiguous():
+            if logits.dim() != 2 or (V > 1 and logits.stride(1) != 1):
+                raise TypeError("logits: only the rows of [rows, vocab] may be strided")
+            if rows > 1:
+                stride = logits.stride(0)
+        f32, i32 = torch.float32, torch.int32
+        ins = [_is(u, f32, rows, "u"), _is(temperature, f32, rows, "temperature"), _is(top_k, i32, rows, "top_k"),
+               _is(top_p, f32, rows, "top_p"), _is(min_p, f32, rows, "min_p")]
+        token = torch.empty(shape, dtype=i32, device=self.device) if token is None else token
+        prob = torch.empty(shape, dtype=f32, device=self.device) if prob is None else prob
+        entropy = torch.empty(shape, dtype=f32, device=self.device) if entropy is None else entropy
+        n_kept = torch.empty(shape, dtype=i32, device=self.device) if n_kept is None else n_kept
+        code = self.lib.sdlm_sample(self.ctx, rows, V, LOGITS_F32 if logits.dtype is f32 else LOGITS_BF16, logits.data_ptr(), stride,
+                                    *ins, _is(token, i32, rows, "token"), _is(prob, f32, rows, "prob"),
+                                    _is(entropy, f32, rows, "entropy"), _is(n_kept, i32, rows, "n_kept"), _stream_ptr(stream))
+        if code:
+            self._check("sdlm_sample", code)
+        return token, prob, entropy, n_kept
 
     def lmhead_confidence_static(self, hidden: torch.Tensor, w_lm: torch.Tensor, token: torch.Tensor,
                                  p_top1: torch.Tensor, entropy: torch.Tensor, max_logit: Optional[torch.Tensor] = None,

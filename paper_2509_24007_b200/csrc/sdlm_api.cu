@@ -647,6 +647,7 @@ extern "C" sdlm_status sdlm_create(const sdlm_config* cfg, void* kv_pool, size_t
   ctx->tmap_w_ptr = nullptr;
   ctx->tmap_w_rows = 0;
   ctx->tmap_h_ptr = nullptr;
+  ctx->rope_rot = 0;
   ctx->defer_merge = 0;
   ctx->pending_merge_fn = nullptr;
   ctx->tmap_h_rows = ctx->tmap_h_box = 0;

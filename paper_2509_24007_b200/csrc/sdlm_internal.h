@@ -98,6 +98,11 @@ struct sdlm_ctx {
   int defer_merge;
   cudaError_t (*pending_merge_fn)(sdlm_ctx*, cudaStream_t);
   alignas(16) unsigned char pending_merge[256];
+  // frequencies of the last sdlm_qk_norm_rope (keyed by its description and head size; 64 powers are 3 us of the host's)
+  sdlm_rope rope_of;
+  int rope_rot;  // 0: none yet
+  float rope_mscale;
+  double rope_freq[64];
   // and of the LM head's hidden-state rows (keyed by pointer, rows and box rows)
   const void* tmap_h_ptr;
   int tmap_h_rows, tmap_h_box;

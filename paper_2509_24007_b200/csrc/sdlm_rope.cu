@@ -17,6 +17,7 @@
 #include "sdlm_ptx.cuh"
 
 #include <math.h>
+#include <string.h>
 
 namespace sdlm {
 
@@ -255,8 +256,15 @@ extern "C" sdlm_status sdlm_qk_norm_rope(sdlm_ctx* ctx, int32_t batch, int32_t D
   p.q_stride = q_stride; p.k_stride = k_stride; p.rows = rows;
   p.D = D; p.max_batch = ctx->cfg.max_batch; p.n_heads = n_heads; p.n_heads2 = n_heads2;
   p.rot = rot; p.interleaved = rope->interleaved; p.eps = eps;
-  for (double& f : p.freq) f = 0.0;
-  if (!rope_frequencies(*rope, rot, p.freq, &p.mscale)) return SDLM_ERR_INVALID_ARG;
+  if (ctx->rope_rot != rot || memcmp(&ctx->rope_of, rope, sizeof(*rope)) != 0) {
+    ctx->rope_rot = 0;
+    for (double& f : ctx->rope_freq) f = 0.0;
+    if (!rope_frequencies(*rope, rot, ctx->rope_freq, &ctx->rope_mscale)) return SDLM_ERR_INVALID_ARG;
+    ctx->rope_of = *rope;
+    ctx->rope_rot = rot;
+  }
+  memcpy(p.freq, ctx->rope_freq, sizeof(p.freq));
+  p.mscale = ctx->rope_mscale;
   const int hpw = 32 / (d / 16), groups = (n_heads + n_heads2 + hpw - 1) / hpw;
   // few rows: one warp for every group of heads; many: fewer warps a row, which then form the angles less often
   const long long want = (long long)ctx->sm_count * 32;

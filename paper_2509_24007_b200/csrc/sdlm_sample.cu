@@ -11,10 +11,17 @@
 // Every filter keeps a prefix of the order, so the kept tokens are those above one key and the first few that equal
 // it, and nothing has to be sorted.
 //
-// What bounds it is reading the logits once.  A cluster of up to eight thread blocks takes a row, a slice each, which
-// stays in shared memory as order-preserving integer keys; all passes after the first run on chip and meet through
-// the cluster's shared memory.  A threshold is found by histograms: first over bins of T/32 below the maximum, where
-// few neighbours collide, then over the keys of the bin that the threshold falls in, until a bin holds one key.
+// What bounds it is reading the logits once and, where many tokens are kept, forming their weights.  A cluster of up to
+// eight thread blocks takes a row, a slice each, which stays in shared memory; the passes after the first run on chip
+// and meet through the cluster's shared memory:
+//   1. the slice is loaded, its maximum taken;
+//   2. (top-k, top-p) tokens are counted by distance from the maximum in bins of T/102: top-k's threshold lies in one bin,
+//      and since a bin's weights are known to 1 %, top-p's in a window of a few;
+//   3. (top-p) one pass forms the weights and adds them up above, in and below that window;
+//   4. thresholds are narrowed down to one value among the few tokens of the bin or window, which were listed on the way;
+//   5. without top-p one pass forms the kept weights; every thread block then knows the weight of all slices, and the one
+//      that holds u W finds its token.
+// -inf and NaN fail every comparison below, so they need no mask of their own.
 //
 // The answer is a comparison of sums of up to 2^18 weights with u W or p times their total, and a token changes when a
 // border moves by a millionth, so weights are formed in 64 bits and summed as whole multiples of 2^-45 (W < 2^18 then
@@ -28,7 +35,10 @@ namespace sdlm {
 
 constexpr int kSampleThreads = 512;
 constexpr int kSampleWarps = kSampleThreads / 32;
-constexpr int kSampleBins = 1024;
+constexpr int kSampleBins = 2048;                 // of distance from the maximum: T/102 each, the last one open
+constexpr int kSampleGroups = kSampleBins / 32;   // sums over 32 bins: what thread blocks tell each other first
+constexpr int kSampleSub = 128;                   // parts a key range is cut into
+constexpr int kSampleList = 2048;                 // tokens of a bin or window that a thread block lists
 constexpr int kSampleMaxVocab = 1 << 18;
 
 struct SampleParams {
@@ -43,90 +53,85 @@ struct SampleParams {
   float* prob;
   float* entropy;
   int32_t* kept;
-  int V, per, seg, vec;      // vocabulary, slice of a thread block, slice of a thread, 16-byte loads
+  int V, per, vec;           // vocabulary, slice of a thread block, 16-byte loads
 };
 
-// A row's slice in shared memory as keys that order like the values: key 0 for a token that cannot be taken (-inf or
-// NaN); +inf counts as the largest finite value, -0 as 0.
+// Keys that order like the values, 32 or 16 bits wide as the logits are (0 and -0 have one).
 template <bool F32>
-struct SampleKey;
-template <>
-struct SampleKey<true> {
-  using type = uint32_t;
-  static __device__ __forceinline__ uint32_t of(uint32_t bits) {
-    if ((bits & 0x7fffffffu) > 0x7f800000u || bits == 0xff800000u) return 0u;
-    if (bits == 0x7f800000u) bits = 0x7f7fffffu;
-    if (bits == 0x80000000u) bits = 0u;
-    return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
-  }
-  static __device__ __forceinline__ float value(uint32_t key) {
-    return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
-  }
-};
-template <>
-struct SampleKey<false> {
-  using type = uint16_t;
-  static __device__ __forceinline__ uint32_t of(uint32_t bits) {
-    if ((bits & 0x7fffu) > 0x7f80u || bits == 0xff80u) return 0u;
-    if (bits == 0x7f80u) bits = 0x7f7fu;
-    if (bits == 0x8000u) bits = 0u;
-    return bits & 0x8000u ? ~bits & 0xffffu : bits | 0x8000u;
-  }
-  static __device__ __forceinline__ float value(uint32_t key) {
-    return __uint_as_float((key & 0x8000u ? key ^ 0x8000u : ~key & 0xffffu) << 16);
-  }
-};
-
-// Weight of a value: t = z log2 e, w = 2^t with a relative error below 1e-11, and w as a multiple of 2^-45.
-struct SampleWeight {
-  double t, w;
-  uint64_t fix;
-};
-__device__ __forceinline__ SampleWeight sample_weight(float v, double vmax, double scale) {
-  SampleWeight r;
-  r.t = fmax(((double)v - vmax) * scale, -300.0);  // 2^-300 is below every positive min_p and adds nothing
-  const double kMagic = 6755399441055744.0;        // 1.5 * 2^52: adding it leaves round(t) in the low bits
-  const double m = r.t + kMagic;
-  const double f = r.t - (m - kMagic);             // |f| <= 1/2
-  // 2^f = sum (f ln 2)^i / i! up to i = 9; what the series leaves out is below (ln 2 / 2)^10 / 10! = 7e-12
-  const double x = f * 0.69314718055994530942;
-  double q = 1.0 / 362880.0;
-  q = fma(q, x, 1.0 / 40320.0);
-  q = fma(q, x, 1.0 / 5040.0);
-  q = fma(q, x, 1.0 / 720.0);
-  q = fma(q, x, 1.0 / 120.0);
-  q = fma(q, x, 1.0 / 24.0);
-  q = fma(q, x, 1.0 / 6.0);
-  q = fma(q, x, 0.5);
-  q = fma(q, x, 1.0);
-  q = fma(q, x, 1.0);
-  r.w = __hiloint2double(__double2hiint(q) + (__double2loint(m) << 20), __double2loint(q));
-  // w 2^45 rounded to a whole number: it is at most 2^45, so adding 2^52 leaves it in the mantissa
-  r.fix = (uint64_t)__double_as_longlong(fma(r.w, 35184372088832.0, 4503599627370496.0)) & 0xfffffffffffffull;
-  return r;
+__device__ __forceinline__ uint32_t sample_key(float v) {
+  const uint32_t b = __float_as_uint(v + 0.0f);
+  const uint32_t k = b & 0x80000000u ? ~b : b | 0x80000000u;
+  return F32 ? k : k >> 16;
+}
+template <bool F32>
+__device__ __forceinline__ float sample_value(uint32_t key) {
+  if (F32) return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+  return __uint_as_float((key & 0x8000u ? key ^ 0x8000u : ~key & 0xffffu) << 16);
 }
 
-// What a thread block tells the others of its cluster.
-struct SampleExchange {
-  uint64_t mass;
-  double wt;       // sum of w t over the kept tokens above the threshold key
-  uint32_t count, ties, max_key, pad;
+// Weight of a value: t = z log2 e (0 at the maximum; -200 below v_floor, and 2^-200 adds nothing) and w = 2^t, with a relative
+// error below 6e-12, as a whole multiple of 2^-45, in a double.
+struct SampleWeight {
+  double t, w45;
 };
+constexpr double kSampleWhole = 4503599627370496.0;  // 2^52: adding it leaves the nearest whole number in the mantissa
+__device__ __forceinline__ SampleWeight sample_weight(float v, float v_floor, double vmax, double scale) {
+  SampleWeight r;
+  r.t = v >= v_floor ? ((double)v - vmax) * scale : -200.0;  // (a NaN is not)
+  const double m = r.t + 1.5 * kSampleWhole;       // round(t) in the low bits
+  const double f = r.t - (m - 1.5 * kSampleWhole); // |f| <= 1/2
+  // 2^f = sum (f ln 2)^i / i! up to i = 7; what the series leaves out is below (ln 2 / 2)^8 / 8! = 5.2e-12
+  double q = 1.5252733804059840e-05;
+  q = fma(q, f, 1.5403530393381609e-04);
+  q = fma(q, f, 1.3333558146428443e-03);
+  q = fma(q, f, 9.6181291076284772e-03);
+  q = fma(q, f, 5.5504108664821580e-02);
+  q = fma(q, f, 2.4022650695910071e-01);
+  q = fma(q, f, 6.9314718055994531e-01);
+  q = fma(q, f, 1.0);
+  const double w45 = __hiloint2double(__double2hiint(q) + ((__double2loint(m) + 45) << 20), __double2loint(q));
+  r.w45 = (w45 + kSampleWhole) - kSampleWhole;     // at most 2^45
+  return r;
+}
+__device__ __forceinline__ uint64_t sample_whole(double x) {  // a whole number below 2^52
+  return (uint64_t)__double_as_longlong(x + kSampleWhole) & 0xfffffffffffffull;
+}
+// -w t as a multiple of 2^-43 (w |t| <= 0.54), for sums whose order is not fixed.
+__device__ __forceinline__ uint64_t sample_entropy(const SampleWeight& w) { return sample_whole(rint(w.w45 * w.t * -0.25)); }
 
-struct alignas(16) SampleShared {  // the keys behind it are read and written 16 bytes at a time
-  uint32_t count[2][kSampleBins];             // by parity of the level: one barrier per level then suffices
-  uint32_t lo[2][kSampleBins], hi[2][kSampleBins];
-  SampleExchange mine;
-  uint64_t scan[kSampleWarps];
-  uint32_t scan32[kSampleWarps];
-  double scan_d[kSampleWarps];
-  uint64_t found_before, total;
-  int found_bin;
-};
-
+// Tokens above `value` are kept, and the first `take` by index of those that equal it.
 struct SampleCut {
-  uint32_t key, take;  // tokens above `key` are kept, and the first `take` of those that equal it
+  float value;
+  uint32_t take;
 };
+
+// Sums over kept tokens.
+struct SampleSums {
+  uint64_t mass;
+  double ent;  // sum of -w t, multiples of 2^-45
+  uint32_t count, ties;
+};
+
+struct alignas(16) SampleShared {  // the values behind it are read and written 16 bytes at a time
+  uint32_t count[kSampleBins + 4];                // the last for tokens that cannot be taken
+  uint32_t group_n[kSampleGroups];                // tokens of 32 bins, and bounds of their weight
+  uint64_t group_lo[kSampleGroups], group_hi[kSampleGroups];
+  uint32_t lo[2][kSampleSub], hi[2][kSampleSub];  // by parity of the level: one barrier per level then suffices
+  uint32_t list[kSampleList];                     // values (bits) of the tokens in question
+  SampleSums mine, extra;                         // what a thread block tells the others of its cluster
+  uint64_t window, below;
+  SampleSums warp[kSampleWarps];
+  uint64_t scan[kSampleWarps], scan2[kSampleWarps];
+  uint32_t scan32[kSampleWarps];
+  uint64_t found_before;
+  float max_value;
+  int found, n_list;
+  // what the first warp finds in the counts
+  int b_k, b0, b1;
+  uint32_t in_k;
+  uint64_t before_k;
+};
+static_assert(sizeof(SampleShared) % 16 == 0, "the values start on a 16-byte boundary");
 
 // Exclusive prefix of v over the thread block in thread order, and the total; all threads call it.
 __device__ __forceinline__ uint64_t sample_scan(uint64_t v, uint64_t* warp_sums, uint64_t& total) {
@@ -149,190 +154,393 @@ __device__ __forceinline__ uint64_t sample_scan(uint64_t v, uint64_t* warp_sums,
   __syncthreads();  // warp_sums may be written again
   return before + incl - v;
 }
+template <typename N>
+__device__ __forceinline__ N sample_warp_sum(N v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
 
 template <bool F32>
 struct SampleRow {
-  using Key = typename SampleKey<F32>::type;
-  const Key* keys;
+  static constexpr int kVec = F32 ? 4 : 8;  // values in 16 bytes
+  const uint4* vals;                         // the slice, -inf behind its end
   SampleShared* sh;
-  int n_pad, C, rank;
-  double vmax, scale;       // largest value; log2 e / T
-  float vmaxf, bin_scale;
-  uint32_t kmax;
-  int level;                // histogram levels so far (buffer parity)
+  int n_vec, C, rank;
+  double scale;                              // log2 e / T
+  float vmax, v_floor, bin_scale;
+  int level;                                 // key levels so far (buffer parity)
 
-  __device__ __forceinline__ int bin_of(float v) const { return min(kSampleBins - 1, __float2int_rz((vmaxf - v) * bin_scale)); }
+  static __device__ __forceinline__ void unpack(const uint4& q, float (&v)[kVec]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (F32) {
+        v[i] = __uint_as_float(w[i]);
+      } else {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    }
+  }
+  // Bin b holds the values about (b - 1/2 .. b + 1/2) / bin_scale below the maximum: the distance, rounded by adding 2^23.
+  __device__ __forceinline__ int bin_of(float v) const {
+    return __float_as_int(fminf((vmax - v) * bin_scale, (float)(kSampleBins - 1)) + 8388608.0f) - 0x4b000000;
+  }
+  __device__ __forceinline__ SampleWeight weight(float v) const { return sample_weight(v, v_floor, (double)vmax, scale); }
 
-  // Finds the cut that leaves the first k tokens (MASS false; want = k) or the shortest prefix with `frac` of the weight
-  // (MASS true), among the tokens above floor.key and the first floor.take that equal it.  Returns false when
-  // nothing is cut off.
+  // Bounds of the weight of n tokens of bin b, as multiples of 2^-40 rounded outwards.  The factors 1 -+ 1e-5 cover what
+  // rounding the distance, which is up to the bin's number, and the powers of two may be off by.
+  __device__ __forceinline__ void bounds(int b, uint32_t n, uint64_t& lo, uint64_t& hi) const {
+    const double kappa = scale / (double)bin_scale;  // log2 units a bin
+    const float near = b == 0 ? 1.0f : exp2f((float)(-((double)b - 0.5) * kappa)) * 1.00001f;
+    const float far = b == kSampleBins - 1 ? 0.0f : exp2f((float)(-((double)b + 0.5) * kappa)) * 0.99999f;
+    lo = (uint64_t)((double)n * (double)far * 1099511627776.0);
+    hi = n ? (uint64_t)((double)n * (double)near * 1099511627776.0) + 1u : 0u;
+  }
+  // Tokens of bin 32 g + lane in the whole cluster; whole warps.
+  __device__ __forceinline__ uint32_t cluster_bin(int g) const {
+    uint32_t n = 0;
+    for (int r = 0; r < C; ++r) n += ptx::ld_cluster_u32(ptx::mapa_u32(ptx::smem_u32(&sh->count[32 * g + (threadIdx.x & 31)]), r));
+    return n;
+  }
+  template <typename N>
+  static __device__ __forceinline__ N warp_prefix(N v) {  // inclusive
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const N w = __shfl_up_sync(0xffffffffu, v, o);
+      if ((threadIdx.x & 31) >= o) v += w;
+    }
+    return v;
+  }
+  // Counts the tokens by bin and finds top-k's bin (b_k, with before_k tokens before it and in_k of it kept) and top-p's
+  // window of bins [b0, b1].  The histograms stay where they are: the thread blocks exchange sums over 32 bins and then only
+  // the bins in question (all of them from all of the others cost more than everything else together).
+  __device__ __forceinline__ void find_bins(bool by_k, int k, bool by_p, double p64) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int i = threadIdx.x; i < kSampleBins / 4; i += kSampleThreads) reinterpret_cast<uint4*>(sh->count)[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    for (int i = threadIdx.x; i < n_vec; i += kSampleThreads) {
+      float v[kVec];
+      unpack(vals[i], v);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) atomicAdd(&sh->count[v[e] > -INFINITY ? bin_of(v[e]) : kSampleBins], 1u);
+    }
+    __syncthreads();
+    for (int g = warp; g < kSampleGroups; g += kSampleWarps) {
+      const uint32_t n = sh->count[32 * g + lane], all = __reduce_add_sync(0xffffffffu, n);
+      uint64_t lo = 0, hi = 0;
+      if (by_p && all) {
+        bounds(32 * g + lane, n, lo, hi);
+        lo = sample_warp_sum(lo);
+        hi = sample_warp_sum(hi);
+      }
+      if (lane == 0) {
+        sh->group_n[g] = all;
+        sh->group_lo[g] = lo;
+        sh->group_hi[g] = hi;
+      }
+    }
+    ptx::cluster_sync_all();
+    if (warp == 0) {
+      static_assert(kSampleGroups == 64, "two groups a lane");
+      uint32_t n[2] = {0, 0};
+      uint64_t lo[2] = {0, 0}, hi[2] = {0, 0};
+      for (int r = 0; r < C; ++r) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          n[i] += ptx::ld_cluster_u32(ptx::mapa_u32(ptx::smem_u32(&sh->group_n[2 * lane + i]), r));
+          if (by_p) {
+            lo[i] += ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->group_lo[2 * lane + i]), r));
+            hi[i] += ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->group_hi[2 * lane + i]), r));
+          }
+        }
+      }
+      int b_k = kSampleBins;
+      uint32_t in_k = 0, fine_k = 0;
+      const uint32_t incl = warp_prefix(n[0] + n[1]), tokens = __shfl_sync(0xffffffffu, incl, 31);
+      if (by_k && (uint32_t)k < tokens) {
+        const uint32_t past = __ballot_sync(0xffffffffu, incl >= (uint32_t)k);
+        const int src = __ffs(past) - 1;
+        const uint32_t before = __shfl_sync(0xffffffffu, incl - n[0] - n[1], src), n_0 = __shfl_sync(0xffffffffu, n[0], src);
+        const int g = 2 * src + (before + n_0 >= (uint32_t)k ? 0 : 1);
+        const uint32_t first = before + (g & 1 ? n_0 : 0u);
+        fine_k = cluster_bin(g);
+        const uint32_t f_incl = first + warp_prefix(fine_k);
+        const int at = __ffs(__ballot_sync(0xffffffffu, f_incl >= (uint32_t)k)) - 1;
+        const uint32_t before_k = __shfl_sync(0xffffffffu, f_incl - fine_k, at);
+        b_k = 32 * g + at;
+        in_k = (uint32_t)k - before_k;
+        fine_k = lane < at ? fine_k : lane == at ? in_k : 0u;  // of that group's bins, what top-k keeps
+        if (lane == 0) sh->before_k = before_k;
+        if (by_p) {
+          uint64_t l, h;
+          bounds(32 * g + lane, fine_k, l, h);
+          l = sample_warp_sum(l);
+          h = sample_warp_sum(h);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (2 * lane + i > g) lo[i] = hi[i] = 0;
+            if (2 * lane + i == g) { lo[i] = l; hi[i] = h; }
+          }
+        }
+      }
+      if (lane == 0) {
+        sh->b_k = b_k;
+        sh->in_k = in_k;
+      }
+      if (by_p) {
+        // The threshold's bin is one whose weight from above, with all before, can reach top_p of the total (the first such
+        // bin is b0), and none behind the first whose weight from below must reach it (b1).
+        const uint64_t l_incl = warp_prefix(lo[0] + lo[1]), h_incl = warp_prefix(hi[0] + hi[1]);
+        const double goal_lo = p64 * (double)__shfl_sync(0xffffffffu, l_incl, 31) * (1.0 - 1e-12);
+        const double goal_hi = p64 * (double)__shfl_sync(0xffffffffu, h_incl, 31) * (1.0 + 1e-12) + 1.0;
+        auto locate = [&](const uint64_t (&v)[2], uint64_t inclusive, double goal, bool upper) {
+          const uint32_t past = __ballot_sync(0xffffffffu, inclusive > 0 && (double)inclusive >= goal);
+          if (!past) return kSampleBins - 1;
+          const int src = __ffs(past) - 1;
+          const uint64_t before = __shfl_sync(0xffffffffu, inclusive - v[0] - v[1], src), v_0 = __shfl_sync(0xffffffffu, v[0], src);
+          const int g = 2 * src + (before + v_0 > 0 && (double)(before + v_0) >= goal ? 0 : 1);
+          const uint32_t m = g == b_k >> 5 ? fine_k : cluster_bin(g);
+          uint64_t l, h;
+          bounds(32 * g + lane, m, l, h);
+          const uint64_t x = before + (g & 1 ? v_0 : 0) + warp_prefix(upper ? h : l);
+          const uint32_t at = __ballot_sync(0xffffffffu, x > 0 && (double)x >= goal && (!upper || m));
+          return at ? 32 * g + __ffs(at) - 1 : min(32 * g + 31, kSampleBins - 1);
+        };
+        const int b0 = locate(hi, h_incl, goal_lo, true), b1 = locate(lo, l_incl, goal_hi, false);
+        if (lane == 0) {
+          sh->b0 = b0;
+          sh->b1 = min(max(b0, b1), b_k);
+        }
+      }
+    }
+    __syncthreads();
+  }
+
+  // Lists the tokens of bins [b0, b1] that `floor` keeps whole; n_list is beyond the list's length when they do not fit.
+  __device__ __forceinline__ void put_on_list(float v) {
+    const int at = atomicAdd(&sh->n_list, 1);
+    if (at < kSampleList) sh->list[at] = __float_as_uint(v);
+  }
+  __device__ __forceinline__ void list_bins(int b0, int b1, const SampleCut& floor) {
+    if (threadIdx.x == 0) sh->n_list = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n_vec; i += kSampleThreads) {
+      float v[kVec];
+      unpack(vals[i], v);
+      uint32_t in = 0;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const int b = bin_of(v[e]);
+        in |= v[e] > floor.value && b >= b0 && b <= b1 ? 1u << e : 0u;
+      }
+      while (in) {
+        const int e = __ffs(in) - 1;
+        in &= in - 1;
+        put_on_list(pick(v, e));
+      }
+    }
+    __syncthreads();
+  }
+  // v[e] without an array in local memory
+  static __device__ __forceinline__ float pick(const float (&v)[kVec], int e) {
+    float x = v[0];
+#pragma unroll
+    for (int i = 1; i < kVec; ++i) x = e == i ? v[i] : x;
+    return x;
+  }
+  // f(value) for the tokens listed (of bins [b0, b1] above the floor), from the slice when the list was too short.
+  template <typename F>
+  __device__ __forceinline__ void each_listed(int b0, int b1, const SampleCut& floor, F f) {
+    if (sh->n_list <= kSampleList) {
+      for (int i = threadIdx.x; i < sh->n_list; i += kSampleThreads) f(__uint_as_float(sh->list[i]));
+    } else {
+      for (int i = threadIdx.x; i < n_vec; i += kSampleThreads) {
+        float v[kVec];
+        unpack(vals[i], v);
+#pragma unroll 1
+        for (int e = 0; e < kVec; ++e)
+          if (v[e] > floor.value) {
+            const int b = bin_of(v[e]);
+            if (b >= b0 && b <= b1) f(v[e]);
+          }
+      }
+    }
+  }
+  // A key no smaller (up) or no larger than that of any value on the inner side of v.
+  __device__ __forceinline__ uint32_t key_near(float v, bool up) const {
+    if (isinf(v)) return sample_key<F32>(up ? vmax : F32 ? -3.402823466e38f : -3.3895314e38f);
+    const uint32_t k = sample_key<true>(v);
+    return F32 ? k : up ? (k >> 16) + 1u : k >> 16;
+  }
+
+  // The value at which the tokens listed, taken from the largest down behind `before`, reach `want` (tokens, or weight when
+  // MASS), and how many of the tokens that equal it are needed.  The first floor.take tokens that equal floor.value belong
+  // to the list when with_floor.
   template <bool MASS>
-  __device__ bool cut(uint64_t want, double frac, const SampleCut floor, SampleCut& out) {
-    uint32_t r_lo = 1, r_hi = kmax;
-    int in_bin = -1, shift = 0;
-    uint64_t before = 0;
-    for (int lev = 0; lev < 8; ++lev) {  // a level leaves a 1024th of at most 2^32 keys: five are enough
-      const int buf = level & 1;
-      uint32_t* cnt = sh->count[buf];
+  __device__ SampleCut narrow(int b0, int b1, const SampleCut floor, bool with_floor, uint64_t before, uint64_t want) {
+    const float near = ((float)b0 - 0.5f) / bin_scale, far = ((float)b1 + 0.5f) / bin_scale;
+    const float slack = 1e-6f * (fabsf(vmax) + far) + 1e-37f;  // what rounding may have moved over a bin's border
+    const uint32_t k_max = sample_key<F32>(vmax);
+    uint32_t r_hi = b0 > 0 ? min(k_max, key_near(vmax - near + slack, true)) : k_max;
+    uint32_t r_lo = b1 < kSampleBins - 1 ? max(1u, key_near(vmax - far - slack, false)) : 1u;
+    for (int lev = 0; lev < 8; ++lev) {  // a level leaves a 128th of at most 2^32 keys: five are enough
+      const int buf = level++ & 1;
       uint32_t* lo = sh->lo[buf];
       uint32_t* hi = sh->hi[buf];
-      for (int i = threadIdx.x; i < kSampleBins; i += kSampleThreads) {
-        if (MASS) lo[i] = hi[i] = 0; else cnt[i] = 0;
-      }
-      if (threadIdx.x == 0) sh->found_bin = 0;
+      if (threadIdx.x < kSampleSub) lo[threadIdx.x] = hi[threadIdx.x] = 0;
+      int part = 0;
+      while (((r_hi - r_lo) >> part) >= (uint32_t)kSampleSub) ++part;
+      if (threadIdx.x == 0) sh->found = 0;
       __syncthreads();
-      auto add = [&](uint32_t key, uint32_t n) {
-        const float v = SampleKey<F32>::value(key);
-        int i;
-        if (lev == 0) {
-          i = bin_of(v);
-        } else {
-          if (key < r_lo || key > r_hi || bin_of(v) != in_bin) return;
-          i = (int)((r_hi - key) >> shift);
-        }
+      auto add = [&](float v, uint32_t n) {
+        const uint32_t key = sample_key<F32>(v);
+        if (key < r_lo || key > r_hi) return;
+        const uint32_t i = (r_hi - key) >> part;
         if (MASS) {
-          const uint64_t w = sample_weight(v, vmax, scale).fix * n;
-          if (w == 0) return;
+          const uint64_t w = sample_whole(weight(v).w45) * n;
           // 64 bits in two halves; the carry goes with whoever brought the lower half over
           const uint32_t w_lo = (uint32_t)w, old = atomicAdd(&lo[i], w_lo);
           const uint32_t up = (uint32_t)(w >> 32) + (old + w_lo < old ? 1u : 0u);
           if (up) atomicAdd(&hi[i], up);
         } else {
-          atomicAdd(&cnt[i], n);
+          atomicAdd(&lo[i], n);
         }
       };
-      for (int i = threadIdx.x; i < n_pad; i += kSampleThreads) {
-        const uint32_t key = keys[i];
-        if (key > floor.key) add(key, 1);
-      }
-      if (floor.take && rank == 0 && threadIdx.x == 0) add(floor.key, floor.take);
-      ++level;
+      each_listed(b0, b1, floor, [&](float v) { add(v, 1); });
+      if (with_floor && rank == 0 && threadIdx.x == 0) add(floor.value, floor.take);
       ptx::cluster_sync_all();
-      // two neighbouring bins a thread, summed over the cluster
-      uint64_t v0 = 0, v1 = 0;
-      for (int r = 0; r < C; ++r) {
-        if (MASS) {
-          const uint2 l = ptx::ld_cluster_v2(ptx::mapa_u32(ptx::smem_u32(&lo[2 * threadIdx.x]), r));
-          const uint2 h = ptx::ld_cluster_v2(ptx::mapa_u32(ptx::smem_u32(&hi[2 * threadIdx.x]), r));
-          v0 += ((uint64_t)h.x << 32) + l.x;
-          v1 += ((uint64_t)h.y << 32) + l.y;
-        } else {
-          const uint2 c = ptx::ld_cluster_v2(ptx::mapa_u32(ptx::smem_u32(&cnt[2 * threadIdx.x]), r));
-          v0 += c.x;
-          v1 += c.y;
+      uint64_t v = 0;
+      if (threadIdx.x < kSampleSub) {
+        for (int r = 0; r < C; ++r) {
+          v += ptx::ld_cluster_u32(ptx::mapa_u32(ptx::smem_u32(&lo[threadIdx.x]), r));
+          if (MASS) v += (uint64_t)ptx::ld_cluster_u32(ptx::mapa_u32(ptx::smem_u32(&hi[threadIdx.x]), r)) << 32;
         }
       }
       uint64_t total;
-      const uint64_t e0 = before + sample_scan(v0 + v1, sh->scan, total), e1 = e0 + v0;
-      if (lev == 0) {
-        if (MASS) {
-          const double t = ceil(frac * (double)total);
-          want = t >= (double)total ? total : t < 1.0 ? 1 : (uint64_t)t;
-        } else if (want >= total) {
-          return false;
-        }
+      const uint64_t e = before + sample_scan(v, sh->scan, total);
+      if (e < want && want <= e + v) {
+        sh->found = threadIdx.x;
+        sh->found_before = e;
       }
-      if (e0 < want && want <= e1) { sh->found_bin = 2 * threadIdx.x; sh->found_before = e0; }
-      if (e1 < want && want <= e1 + v1) { sh->found_bin = 2 * threadIdx.x + 1; sh->found_before = e1; }
       __syncthreads();
-      const int bin = sh->found_bin;
+      r_hi -= (uint32_t)sh->found << part;
       before = sh->found_before;
-      __syncthreads();
-      if (lev == 0) {
-        // keys of the bin: values between vmax - (bin + 1) / s and vmax - bin / s, widened by what rounding may move
-        in_bin = bin;
-        const float near = (float)bin / bin_scale, far = (float)(bin + 1) / bin_scale;
-        const float slack = 1e-6f * (fabsf(vmaxf) + far) + 1e-37f;
-        r_hi = kmax;
-        r_lo = 1;
-        if (bin > 0) r_hi = min(kmax, key_near(vmaxf - near + slack, true));
-        if (bin < kSampleBins - 1) r_lo = max(1u, key_near(vmaxf - far - slack, false));
-      } else {
-        r_hi -= (uint32_t)bin << shift;
-        const uint32_t w = (1u << shift) - 1u;
-        r_lo = r_hi - r_lo > w ? r_hi - w : r_lo;
-        if (shift == 0) break;
-      }
-      shift = 0;
-      while (((r_hi - r_lo) >> shift) >= (uint32_t)kSampleBins) ++shift;
+      const uint32_t w = (1u << part) - 1u;
+      r_lo = r_hi - r_lo > w ? r_hi - w : r_lo;
+      __syncthreads();  // found may be written again
+      if (r_hi == r_lo) break;
     }
-    out.key = r_hi;
-    const uint64_t each = MASS ? max((uint64_t)1, sample_weight(SampleKey<F32>::value(r_hi), vmax, scale).fix) : 1;
-    out.take = (uint32_t)((want - before + each - 1) / each);
-    return true;
+    const float value = sample_value<F32>(r_hi);
+    const uint64_t each = MASS ? max((uint64_t)1, sample_whole(weight(value).w45)) : 1;
+    return SampleCut{value, (uint32_t)((want - before + each - 1) / each)};
   }
 
-  // A key no smaller (up) or no larger than that of any value on the inner side of v.
-  __device__ __forceinline__ uint32_t key_near(float v, bool up) const {
-    if (isinf(v)) return up ? kmax : 1u;
-    const uint32_t k = SampleKey<true>::of(__float_as_uint(v));
-    return F32 ? k : up ? (k >> 16) + 1u : k >> 16;
+  // Sums over the slice's tokens above the cut (with t >= min_t), by warp: warp w has a contiguous part of the slice.
+  __device__ __forceinline__ int warp_vecs() const { return (n_vec + kSampleWarps - 1) / kSampleWarps; }
+  __device__ void kept_sums(const SampleCut& cut, double min_t, float reject) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = warp * warp_vecs(), last = min(n_vec, first + warp_vecs());
+    SampleSums s{0, 0.0, 0, 0};
+    for (int i = first + lane; i < last; i += 32) {
+      float v[kVec];
+      unpack(vals[i], v);
+      float mx = v[0];
+#pragma unroll
+      for (int e = 1; e < kVec; ++e) mx = fmaxf(mx, v[e]);
+      if (!(mx >= reject)) continue;
+      // (no branch on a single token: eight chains of 64-bit operations at a time keep their pipe fed, one does not)
+      double sum = kSampleWhole;  // whole numbers, below 2^48 together
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const SampleWeight w = weight(v[e]);
+        const bool in = v[e] > cut.value && v[e] >= reject && w.t >= min_t;
+        const double x = in ? w.w45 : 0.0;
+        sum += x;
+        s.ent = fma(x, -w.t, s.ent);
+        s.count += in ? 1u : 0u;
+        s.ties += v[e] == cut.value && v[e] > -INFINITY ? 1u : 0u;
+      }
+      s.mass += (uint64_t)__double_as_longlong(sum) & 0xfffffffffffffull;
+    }
+    s.mass = sample_warp_sum(s.mass);
+    s.ent = sample_warp_sum(s.ent);
+    s.count = __reduce_add_sync(0xffffffffu, s.count);
+    s.ties = __reduce_add_sync(0xffffffffu, s.ties);
+    if (lane == 0) sh->warp[warp] = s;
+    __syncthreads();
   }
 };
 
 template <bool F32>
-__global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleParams p) {
-  using Key = typename SampleKey<F32>::type;
+__global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleParams p) {
+  using Row = SampleRow<F32>;
+  constexpr int kVec = Row::kVec;
   extern __shared__ __align__(16) uint8_t sample_smem[];
   SampleShared* sh = reinterpret_cast<SampleShared*>(sample_smem);
-  Key* keys = reinterpret_cast<Key*>(sample_smem + sizeof(SampleShared));
+  uint4* vals = reinterpret_cast<uint4*>(sample_smem + sizeof(SampleShared));
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  uint32_t C, rank;
+  uint32_t C;
   asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(C));
-  rank = ptx::cluster_ctarank();
+  const uint32_t rank = ptx::cluster_ctarank();
   const int row = blockIdx.x / C;
   ptx::grid_dep_launch();
   ptx::grid_dep_wait();
+  // the row's parameters, asked for before anything else
+  const float T = p.temperature ? p.temperature[row] : 1.0f;
+  const int k = p.top_k ? p.top_k[row] : 0;
+  const float top_p = p.top_p ? p.top_p[row] : 1.0f;
+  const float mp = p.min_p ? p.min_p[row] : 0.0f;
+  const float u = p.u[row];
 
-  // ---- the slice into shared memory, its largest key
-  const int first = (int)rank * p.per, n = max(0, min(p.per, p.V - first)), n_pad = kSampleThreads * p.seg;
-  uint32_t kmax = 0;
-  if (F32) {
-    const uint32_t* src = static_cast<const uint32_t*>(p.logits) + (long long)row * p.ld + first;
-    const int whole = p.vec ? n / 4 : 0;
-#pragma unroll 4
-    for (int i = tid; i < whole; i += kSampleThreads) {
-      const uint4 v = __ldg(reinterpret_cast<const uint4*>(src) + i);
-      const uint4 k = make_uint4(SampleKey<true>::of(v.x), SampleKey<true>::of(v.y), SampleKey<true>::of(v.z), SampleKey<true>::of(v.w));
-      reinterpret_cast<uint4*>(keys)[i] = k;
-      kmax = max(max(kmax, max(k.x, k.y)), max(k.z, k.w));
-    }
-    for (int i = whole * 4 + tid; i < n_pad; i += kSampleThreads) {
-      const uint32_t k = i < n ? SampleKey<true>::of(src[i]) : 0u;
-      keys[i] = (Key)k;
-      kmax = max(kmax, k);
-    }
-  } else {
-    const uint16_t* src = static_cast<const uint16_t*>(p.logits) + (long long)row * p.ld + first;
-    const int whole = p.vec ? n / 8 : 0;
-#pragma unroll 4
-    for (int i = tid; i < whole; i += kSampleThreads) {
-      const uint4 v = __ldg(reinterpret_cast<const uint4*>(src) + i);
-      const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-      uint32_t out[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t a = SampleKey<false>::of(in[e] & 0xffffu), b = SampleKey<false>::of(in[e] >> 16);
-        out[e] = a | b << 16;
-        kmax = max(kmax, max(a, b));
+  // ---- the slice into shared memory, its largest value
+  const int first = (int)rank * p.per, n = max(0, min(p.per, p.V - first)), n_vec = (n + kVec - 1) / kVec;
+  float mx = -INFINITY;
+  {
+    const int whole = p.vec ? n / kVec : 0;
+    if (F32) {
+      const uint32_t* src = static_cast<const uint32_t*>(p.logits) + (long long)row * p.ld + first;
+#pragma unroll 5
+      for (int i = tid; i < whole; i += kSampleThreads) {
+        const uint4 q = __ldg(reinterpret_cast<const uint4*>(src) + i);
+        vals[i] = q;
+        mx = fmaxf(fmaxf(fmaxf(mx, __uint_as_float(q.x)), fmaxf(__uint_as_float(q.y), __uint_as_float(q.z))), __uint_as_float(q.w));
       }
-      reinterpret_cast<uint4*>(keys)[i] = make_uint4(out[0], out[1], out[2], out[3]);
-    }
-    for (int i = whole * 8 + tid; i < n_pad; i += kSampleThreads) {
-      const uint32_t k = i < n ? SampleKey<false>::of(src[i]) : 0u;
-      keys[i] = (Key)k;
-      kmax = max(kmax, k);
+      uint32_t* dst = reinterpret_cast<uint32_t*>(vals);
+      for (int i = whole * kVec + tid; i < n_vec * kVec; i += kSampleThreads) {
+        const uint32_t b = i < n ? src[i] : 0xff800000u;
+        dst[i] = b;
+        mx = fmaxf(mx, __uint_as_float(b));
+      }
+    } else {
+      const uint16_t* src = static_cast<const uint16_t*>(p.logits) + (long long)row * p.ld + first;
+      __nv_bfloat162 m2 = __floats2bfloat162_rn(-INFINITY, -INFINITY);
+#pragma unroll 5
+      for (int i = tid; i < whole; i += kSampleThreads) {
+        const uint4 q = __ldg(reinterpret_cast<const uint4*>(src) + i);
+        vals[i] = q;
+        const __nv_bfloat162* b = reinterpret_cast<const __nv_bfloat162*>(&q);
+        m2 = __hmax2(m2, __hmax2(__hmax2(b[0], b[1]), __hmax2(b[2], b[3])));
+      }
+      mx = fmaxf(__low2float(m2), __high2float(m2));
+      uint16_t* dst = reinterpret_cast<uint16_t*>(vals);
+      for (int i = whole * kVec + tid; i < n_vec * kVec; i += kSampleThreads) {
+        const uint16_t b = i < n ? src[i] : (uint16_t)0xff80u;
+        dst[i] = b;
+        mx = fmaxf(mx, __uint_as_float((uint32_t)b << 16));
+      }
     }
   }
-  kmax = __reduce_max_sync(0xffffffffu, kmax);
-  if (lane == 0) sh->scan32[warp] = kmax;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));  // a NaN loses against any number
+  if (lane == 0) sh->scan32[warp] = __float_as_uint(mx);
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kSampleWarps; ++i) kmax = max(kmax, sh->scan32[i]);
-  if (tid == 0) sh->mine.max_key = kmax;
+  for (int i = 0; i < kSampleWarps; ++i) mx = fmaxf(mx, __uint_as_float(sh->scan32[i]));
+  if (tid == 0) sh->max_value = mx;
   ptx::cluster_sync_all();
-  for (uint32_t r = 0; r < C; ++r) kmax = max(kmax, ptx::ld_cluster_u32(ptx::mapa_u32(ptx::smem_u32(&sh->mine.max_key), r)));
-  if (kmax == 0) {  // no token can be taken
+  for (uint32_t r = 0; r < C; ++r) mx = fmaxf(mx, __uint_as_float(ptx::ld_cluster_u32(ptx::mapa_u32(ptx::smem_u32(&sh->max_value), r))));
+  if (!(mx > -INFINITY)) {  // no token can be taken
     if (rank == 0 && tid == 0) {
       p.token[row] = -1;
       p.prob[row] = 0.f;
@@ -342,78 +550,203 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SamplePara
     ptx::cluster_sync_all();  // the others may still read this thread block's maximum
     return;
   }
+  if (mx == INFINITY) {  // +inf counts as the largest finite value
+    mx = F32 ? __uint_as_float(0x7f7fffffu) : __uint_as_float(0x7f7f0000u);
+    for (int i = tid; i < n_vec * kVec; i += kSampleThreads) {
+      if (F32) {
+        uint32_t* x = reinterpret_cast<uint32_t*>(vals) + i;
+        if (*x == 0x7f800000u) *x = 0x7f7fffffu;
+      } else {
+        uint16_t* x = reinterpret_cast<uint16_t*>(vals) + i;
+        if (*x == 0x7f80u) *x = 0x7f7fu;
+      }
+    }
+    __syncthreads();
+  }
 
   // ---- thresholds
-  const float T = p.temperature ? p.temperature[row] : 1.0f;
   const bool greedy = !(T > 0.0f);
-  SampleRow<F32> s;
-  s.keys = keys; s.sh = sh; s.n_pad = n_pad; s.C = (int)C; s.rank = (int)rank;
-  s.kmax = kmax; s.level = 0;
-  s.vmaxf = SampleKey<F32>::value(kmax);
-  s.vmax = (double)s.vmaxf;
+  Row s;
+  s.vals = vals; s.sh = sh; s.n_vec = n_vec; s.C = (int)C; s.rank = (int)rank; s.level = 0;
+  s.vmax = mx;
+  s.v_floor = fmaxf(mx - 138.0f * (greedy ? 1.0f : T), -3.402823466e38f);  // 200 ln 2 T below, and no -inf
   s.scale = 1.4426950408889634074 / (double)(greedy ? 1.0f : T);
-  s.bin_scale = (float)kSampleBins / (32.0f * fminf(fmaxf(greedy ? 1.0f : T, 1e-30f), 1e30f));
-  SampleCut cut{0u, 0u};
-  const int k = p.top_k ? p.top_k[row] : 0;
-  if (greedy || k == 1) {
-    cut = SampleCut{kmax, 1u};
-  } else {
-    SampleCut c;
-    if (k > 0 && k < p.V && s.template cut<false>((uint64_t)k, 0.0, cut, c)) cut = c;
-    const float top_p = p.top_p ? p.top_p[row] : 1.0f;
-    if (top_p < 1.0f && s.template cut<true>(0, fmax((double)top_p, 0.0), cut, c)) cut = c;
-  }
-  const float mp = p.min_p ? p.min_p[row] : 0.0f;
-  const double min_w = mp > 0.0f ? fmin((double)mp, 1.0) : -1.0;
-
-  // ---- what is kept, by contiguous slices of the threads
-  uint64_t mass = 0;
-  double wt = 0.0;
-  uint32_t count = 0, ties = 0;
-  const Key* seg = keys + tid * p.seg;
-  for (int i = 0; i < p.seg; ++i) {
-    const uint32_t key = seg[i];
-    if (key > cut.key) {
-      const SampleWeight w = sample_weight(SampleKey<F32>::value(key), s.vmax, s.scale);
-      if (w.w >= min_w) {
-        mass += w.fix;
-        wt = fma(w.w, w.t, wt);
-        ++count;
-      }
-    } else if (key == cut.key && key != 0) {
-      ++ties;
+  s.bin_scale = (float)kSampleBins / (20.0f * fminf(fmaxf(greedy ? 1.0f : T, 1e-30f), 1e30f));
+  SampleCut cut{-INFINITY, 0u};
+  const bool by_k = k > 1 && k < p.V, by_p = top_p < 1.0f;
+  // 0: nothing to find, 1: the first token alone, 2: thresholds.  Opaque to the compiler: nvcc 12.9 takes the branch for 2
+  // out when it can see through the condition, and the filters then keep everything (the tests show it).
+  int mode = greedy || k == 1 ? 1 : by_k || by_p ? 2 : 0;
+  asm volatile("" : "+r"(mode));
+  SampleSums own{0, 0.0, 0, 0};  // this thread block's kept tokens, once known
+  bool summed = false;
+  if (mode == 1) {
+    cut = SampleCut{mx, 1u};
+  } else if (mode == 2) {
+    const double p64 = fmax((double)top_p, 0.0);
+    s.find_bins(by_k, k, by_p, p64);
+    const int b_k = sh->b_k, b0 = sh->b0, b1 = sh->b1;
+    if (b_k < kSampleBins) {
+      s.list_bins(b_k, b_k, cut);
+      cut = s.template narrow<false>(b_k, b_k, cut, false, sh->before_k, (uint64_t)k);
     }
-  }
-  uint64_t cta_mass, cta_ties;
-  const uint64_t mass_before = sample_scan(mass, sh->scan, cta_mass);
-  const uint64_t ties_before = sample_scan(ties, sh->scan, cta_ties);
+    if (by_p) {
+      if (tid == 0) sh->n_list = 0;
+      __syncthreads();
+      const SampleCut top = cut;
+      // one pass over the weights: above the window, in it (listed), below it
+      uint64_t above = 0, inside = 0, below = 0;
+      double ent = 0.0;
+      uint32_t count = 0;
+      for (int i = tid; i < n_vec; i += kSampleThreads) {
+        float v[kVec];
+        Row::unpack(vals[i], v);
+        float most = v[0];
 #pragma unroll
-  for (int o = 16; o; o >>= 1) wt += __shfl_xor_sync(0xffffffffu, wt, o);
-  count = __reduce_add_sync(0xffffffffu, count);
-  if (lane == 0) {
-    sh->scan_d[warp] = wt;
-    sh->scan32[warp] = count;
-  }
-  __syncthreads();
-  if (tid == 0) {
-    SampleExchange x{cta_mass, 0.0, 0u, (uint32_t)cta_ties, kmax, 0u};
-    for (int i = 0; i < kSampleWarps; ++i) {
-      x.wt += sh->scan_d[i];
-      x.count += sh->scan32[i];
+        for (int e = 1; e < kVec; ++e) most = fmaxf(most, v[e]);
+        if (!(most > top.value)) continue;
+        uint32_t listed = 0;
+        double d_up = kSampleWhole, d_mid = kSampleWhole, d_low = kSampleWhole;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+          const SampleWeight w = s.weight(v[e]);
+          const int b = s.bin_of(v[e]);
+          const bool in = v[e] > top.value, up = in && b < b0, mid = in && !up && b <= b1;
+          const double x = up ? w.w45 : 0.0;
+          d_up += x;
+          ent = fma(x, -w.t, ent);
+          d_mid += mid ? w.w45 : 0.0;
+          d_low += in && !up && !mid ? w.w45 : 0.0;
+          count += up ? 1u : 0u;
+          listed |= mid ? 1u << e : 0u;
+        }
+        above += (uint64_t)__double_as_longlong(d_up) & 0xfffffffffffffull;
+        inside += (uint64_t)__double_as_longlong(d_mid) & 0xfffffffffffffull;
+        below += (uint64_t)__double_as_longlong(d_low) & 0xfffffffffffffull;
+        while (listed) {
+          const int e = __ffs(listed) - 1;
+          listed &= listed - 1;
+          s.put_on_list(Row::pick(v, e));
+        }
+      }
+      above = sample_warp_sum(above);
+      ent = sample_warp_sum(ent);
+      inside = sample_warp_sum(inside);
+      below = sample_warp_sum(below);
+      count = __reduce_add_sync(0xffffffffu, count);
+      if (lane == 0) {
+        sh->warp[warp] = SampleSums{above, ent, count, 0u};
+        sh->scan[warp] = inside;
+        sh->scan2[warp] = below;
+      }
+      __syncthreads();
+      if (tid == 0) {
+        SampleSums a{0, 0.0, 0, 0};
+        uint64_t w_in = 0, w_be = 0;
+        for (int i = 0; i < kSampleWarps; ++i) {
+          a.mass += sh->warp[i].mass;
+          a.ent += sh->warp[i].ent;
+          a.count += sh->warp[i].count;
+          w_in += sh->scan[i];
+          w_be += sh->scan2[i];
+        }
+        sh->extra = a;
+        sh->window = w_in;
+        sh->below = w_be;
+      }
+      ptx::cluster_sync_all();
+      uint64_t all_above = 0, all = 0;
+      for (uint32_t r = 0; r < C; ++r) {
+        const uint64_t a = ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->extra.mass), r));
+        all_above += a;
+        all += a + ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->window), r)) +
+               ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->below), r));
+      }
+      const bool tied_k = b_k < kSampleBins;  // top-k kept some of the tokens that equal its threshold (they are not listed)
+      if (tied_k) all += sample_whole(s.weight(top.value).w45) * top.take;
+      const double goal = ceil(p64 * (double)all);
+      const uint64_t want = goal >= (double)all ? all : goal < 1.0 ? 1 : (uint64_t)goal;
+      cut = s.template narrow<true>(b0, b1, top, tied_k && b_k <= b1, all_above, want);
+      if (tied_k && cut.value == top.value) cut.take = min(cut.take, top.take);
+      // this thread block's kept tokens: those above the window and the listed ones above the cut
+      uint64_t m2 = 0, e2 = 0;
+      uint32_t c2 = 0, t2 = 0;
+      s.each_listed(b0, b1, top, [&](float v) {
+        if (v > cut.value) {
+          const SampleWeight w = s.weight(v);
+          m2 += sample_whole(w.w45);
+          e2 += sample_entropy(w);
+          ++c2;
+        } else if (v == cut.value) {
+          ++t2;
+        }
+      });
+      if (tied_k && cut.value == top.value) {  // (these were not listed)
+        for (int i = tid; i < n_vec; i += kSampleThreads) {
+          float v[kVec];
+          Row::unpack(vals[i], v);
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) t2 += v[e] == cut.value ? 1u : 0u;
+        }
+      }
+      m2 = sample_warp_sum(m2);
+      e2 = sample_warp_sum(e2);
+      c2 = __reduce_add_sync(0xffffffffu, c2);
+      t2 = __reduce_add_sync(0xffffffffu, t2);
+      if (lane == 0) sh->warp[warp] = SampleSums{m2, 4.0 * (double)e2, c2, t2};  // (the sums over the list in whole numbers)
+      __syncthreads();
+      own = sh->extra;
+#pragma unroll 1
+      for (int i = 0; i < kSampleWarps; ++i) {
+        own.mass += sh->warp[i].mass;
+        own.ent += sh->warp[i].ent;
+        own.count += sh->warp[i].count;
+        own.ties += sh->warp[i].ties;
+      }
+      summed = true;
     }
-    sh->mine = x;  // (whoever still reads max_key gets the cluster's maximum, which does as well)
   }
+  // w >= min_p as t >= log2 min_p; `reject`: a value that no kept token is below
+  double min_t = -INFINITY;
+  float reject = cut.value;
+  if (mp > 0.0f) {
+    min_t = log2(fmin((double)mp, 1.0));
+    if (cut.value > -INFINITY && s.weight(cut.value).t >= min_t) {
+      min_t = -INFINITY;  // the cut already stands above it
+    } else {
+      summed = false;
+      const double down = min_t / s.scale;
+      reject = fmaxf(reject, (float)((double)mx + down - 1e-6 * (fabs((double)mx) - down)));
+    }
+  }
+
+  // ---- what is kept in each slice
+  bool warps_known = false;
+  if (!summed) {
+    s.kept_sums(cut, min_t, reject);
+    warps_known = true;
+    own = SampleSums{0, 0.0, 0, 0};
+#pragma unroll 1
+    for (int i = 0; i < kSampleWarps; ++i) {
+      own.mass += sh->warp[i].mass;
+      own.ent += sh->warp[i].ent;
+      own.count += sh->warp[i].count;
+      own.ties += sh->warp[i].ties;
+    }
+  }
+  if (tid == 0) sh->mine = own;
   ptx::cluster_sync_all();
-  const SampleWeight tie = sample_weight(SampleKey<F32>::value(cut.key), s.vmax, s.scale);
-  const uint64_t tie_fix = cut.key ? tie.fix : 0;
-  uint32_t take = cut.key && tie.w >= min_w ? cut.take : 0u;
+  const bool has_cut = cut.value > -INFINITY;
+  const SampleWeight tie = s.weight(has_cut ? cut.value : mx);
+  const uint64_t tie_fix = has_cut ? sample_whole(tie.w45) : 0;
+  uint32_t take = has_cut && tie.t >= min_t ? cut.take : 0u;
   uint64_t W = 0, my_first = 0, my_mass = 0;
+  double sum_ent = 0.0;
   uint32_t my_take = 0, kept = 0;
-  double sum_wt = 0.0;
   for (uint32_t r = 0; r < C; ++r) {
     const uint32_t a = ptx::mapa_u32(ptx::smem_u32(&sh->mine), r);
-    const uint64_t m = ptx::ld_cluster_u64(a + offsetof(SampleExchange, mass));
-    const uint32_t t = min(take, ptx::ld_cluster_u32(a + offsetof(SampleExchange, ties)));
+    const uint64_t m = ptx::ld_cluster_u64(a + offsetof(SampleSums, mass));
+    const uint32_t t = min(take, ptx::ld_cluster_u32(a + offsetof(SampleSums, ties)));
     const uint64_t all = m + (uint64_t)t * tie_fix;
     if (r == rank) {
       my_first = W;
@@ -422,65 +755,95 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SamplePara
     }
     W += all;
     take -= t;
-    kept += ptx::ld_cluster_u32(a + offsetof(SampleExchange, count)) + t;
-    sum_wt += __longlong_as_double((long long)ptx::ld_cluster_u64(a + offsetof(SampleExchange, wt))) + (double)t * (cut.key ? tie.w * tie.t : 0.0);
+    kept += ptx::ld_cluster_u32(a + offsetof(SampleSums, count)) + t;
+    sum_ent += __longlong_as_double((long long)ptx::ld_cluster_u64(a + offsetof(SampleSums, ent)));
+    if (has_cut) sum_ent = fma((double)t, -tie.w45 * tie.t, sum_ent);
   }
   ptx::cluster_sync_all();  // nothing of another thread block is read after this
 
   // ---- the token
-  const float u = p.u[row];
   const double at = floor((u > 0.0f ? (double)u : 0.0) * (double)W);
   const uint64_t target = at >= (double)(W - 1) ? W - 1 : (uint64_t)at;
   if (rank == 0 && tid == 0) {
-    const double total = (double)W * (1.0 / 35184372088832.0);
-    p.entropy[row] = fmaxf(0.0f, (float)(log(total) - 0.69314718055994530942 * sum_wt / total));
+    const double total = (double)W * (1.0 / 35184372088832.0);  // 2^45
+    p.entropy[row] = fmaxf(0.0f, (float)(log(total) + 0.69314718055994530942 * sum_ent * (1.0 / 35184372088832.0) / total));
     if (p.kept) p.kept[row] = (int32_t)kept;
   }
   if (target < my_first || target >= my_first + my_mass) return;
-  const uint64_t rest = target - my_first;
-  const uint32_t t_before = (uint32_t)min((uint64_t)my_take, ties_before);
-  const uint64_t start = mass_before + (uint64_t)t_before * tie_fix;
-  const uint64_t own = mass + (uint64_t)min(my_take - t_before, ties) * tie_fix;
-  const uint32_t who = __ballot_sync(0xffffffffu, rest >= start && rest < start + own);
-  if (!who) return;
-  // the warp goes through that thread's slice together, 32 tokens at a time
-  const int src = __ffs(who) - 1;
-  uint64_t left = rest - __shfl_sync(0xffffffffu, start, src);
-  uint32_t t_left = my_take - __shfl_sync(0xffffffffu, t_before, src);
-  const int base = (warp * 32 + src) * p.seg;
-  for (int i0 = 0; i0 < p.seg; i0 += 32) {
-    const uint32_t key = i0 + lane < p.seg ? keys[base + i0 + lane] : 0u;
-    const uint32_t eq = __ballot_sync(0xffffffffu, key == cut.key && key != 0);
-    uint64_t w = 0;
-    if (key > cut.key) {
-      const SampleWeight x = sample_weight(SampleKey<F32>::value(key), s.vmax, s.scale);
-      if (x.w >= min_w) w = x.fix;
-    } else if ((eq >> lane & 1u) && __popc(eq & ((1u << lane) - 1u)) < t_left) {
-      w = tie_fix;
+  uint64_t rest = target - my_first;
+  if (!warps_known) s.kept_sums(cut, min_t, reject);
+  // the warp whose part holds it
+  uint32_t t_left = my_take;
+  int w = 0;
+  for (; w < kSampleWarps - 1; ++w) {
+    const uint32_t t = min(t_left, sh->warp[w].ties);
+    const uint64_t m = sh->warp[w].mass + (uint64_t)t * tie_fix;
+    if (rest < m) break;
+    rest -= m;
+    t_left -= t;
+  }
+  if (w != warp) return;
+  const int v_first = warp * s.warp_vecs(), v_last = min(n_vec, v_first + s.warp_vecs());
+  for (int i0 = v_first; i0 < v_last; i0 += 32) {
+    float v[kVec];
+    uint64_t m[kVec], mass = 0;
+    uint32_t ties = 0;
+    if (i0 + lane < v_last) {
+      Row::unpack(vals[i0 + lane], v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) v[e] = -INFINITY;
     }
-    uint64_t incl = w;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      const SampleWeight x = s.weight(v[e]);
+      m[e] = v[e] > cut.value && x.t >= min_t ? sample_whole(x.w45) : 0;
+      ties += v[e] == cut.value && has_cut ? 1u : 0u;
+      mass += m[e];
+    }
+    uint32_t t_incl = ties;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, t_incl, o);
+      if (lane >= o) t_incl += x;
+    }
+    uint32_t t_mine = t_left > t_incl - ties ? min(ties, t_left - (t_incl - ties)) : 0u;  // of this lane's, the first so many
+    uint64_t incl = mass + (uint64_t)t_mine * tie_fix;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const uint64_t x = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += x;
     }
-    const uint32_t past = __ballot_sync(0xffffffffu, incl > left);
+    const uint32_t past = __ballot_sync(0xffffffffu, incl > rest);
     if (past) {
-      if (lane == __ffs(past) - 1) {
-        p.token[row] = first + base + i0 + lane;
-        p.prob[row] = (float)((double)w / (double)W);
+      const int src = __ffs(past) - 1;
+      const uint64_t before = __shfl_sync(0xffffffffu, incl, src > 0 ? src - 1 : 0);
+      if (lane == src) {
+        uint64_t left = rest - (src > 0 ? before : 0);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+          uint64_t x = m[e];
+          if (v[e] == cut.value && has_cut && t_mine) {
+            x = tie_fix;
+            --t_mine;
+          }
+          if (left < x) {
+            p.token[row] = first + (i0 + lane) * kVec + e;
+            p.prob[row] = (float)((double)x / (double)W);
+            break;
+          }
+          left -= x;
+        }
       }
       return;
     }
-    left -= __shfl_sync(0xffffffffu, incl, 31);
-    t_left -= min(t_left, (uint32_t)__popc(eq));
+    rest -= __shfl_sync(0xffffffffu, incl, 31);
+    t_left -= min(t_left, __shfl_sync(0xffffffffu, t_incl, 31));
   }
 }
 
-static_assert(sizeof(SampleShared) % 16 == 0, "the keys start on a 16-byte boundary");
-
 cudaError_t setup_sample(sdlm_ctx*) {
-  const int most = (int)sizeof(SampleShared) + (kSampleMaxVocab / 8 + 2 * kSampleThreads) * 4;
+  const int most = (int)sizeof(SampleShared) + (kSampleMaxVocab / 8 + 8) * 4;
   cudaError_t e = cudaFuncSetAttribute(sample_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(sample_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
   return e;
@@ -507,16 +870,16 @@ extern "C" sdlm_status sdlm_sample(sdlm_ctx* ctx, int32_t rows, int32_t vocab, s
   p.logits = logits; p.ld = row_stride; p.u = u; p.temperature = temperature; p.top_k = top_k; p.top_p = top_p; p.min_p = min_p;
   p.token = token; p.prob = prob; p.entropy = entropy; p.kept = n_kept;
   p.V = vocab;
-  // one thread block for every 8192 tokens or so, in powers of two up to eight (the portable cluster size)
-  unsigned c = 1;
-  while (c < 8 && vocab > 8192 * (int)c) c *= 2;
-  p.per = (int)(((vocab + c - 1) / c + 7) / 8 * 8);
-  // a thread's slice is an odd number of 32-bit words, so that the threads of a warp start in different banks
-  const int words = f32 ? (p.per + kSampleThreads - 1) / kSampleThreads : (p.per + 2 * kSampleThreads - 1) / (2 * kSampleThreads);
-  p.seg = (words | 1) * (f32 ? 1 : 2);
+  // Thread blocks of a row, in powers of two up to eight (the portable cluster size): a slice of at most 80 KB, so that two
+  // fit an SM, and eight where all rows then run at once.  More of them have less to do each but meet as often: 128 rows of
+  // 151936 bf16 logits, top-k: 65 us with four, 138 with eight; one row: 28 and 25.
   const int esz = f32 ? 4 : 2;
+  unsigned c = 1;
+  const int most = rows * 8 <= ctx->sm_count ? 16384 : 81920;
+  while (c < 8 && (long long)vocab * esz > (long long)most * c) c *= 2;
+  p.per = (int)(((vocab + c - 1) / c + 7) / 8 * 8);
   p.vec = at % 16 == 0 && (row_stride * esz) % 16 == 0;
-  const size_t smem = sizeof(SampleShared) + (size_t)kSampleThreads * p.seg * esz;
+  const size_t smem = sizeof(SampleShared) + (size_t)p.per * esz;
   const dim3 grid((unsigned)rows * c);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e = f32 ? launch_overlapped_cluster(sample_kernel<true>, grid, dim3(kSampleThreads), smem, st, c, p)
