@@ -782,11 +782,11 @@ class Sdlm:
         batch, n = shape = self._tree_shape(parent)
         i32 = torch.int32
         if accepted_len is None:
-            accepted_len = torch.empty(batch, dtype=i32, device=self.device)
+            accepted_len = parent.new_empty(batch)
         if out_tokens is None:
-            out_tokens = torch.empty(shape, dtype=i32, device=self.device)
+            out_tokens = torch.empty_like(parent)
         if path is None:
-            path = torch.empty(shape, dtype=i32, device=self.device)
+            path = torch.empty_like(parent)
         before = [_is(seq_ids, i32, batch, "seq_ids"), _is(n_nodes, i32, batch, "n_nodes"), _shaped(parent, i32, shape, "parent"),
                   _shaped(draft_token, i32, shape, "draft_token"), _shaped(next_token, i32, shape, "next_token")]
         after = [_is(accepted_len, i32, batch, "accepted_len"), _shaped(out_tokens, i32, shape, "out_tokens"),
@@ -838,10 +838,10 @@ class Sdlm:
         f32, i32 = torch.float32, torch.int32
         ins = [_is(u, f32, rows, "u"), _is(temperature, f32, rows, "temperature"), _is(top_k, i32, rows, "top_k"),
                _is(top_p, f32, rows, "top_p"), _is(min_p, f32, rows, "min_p")]
-        token = torch.empty(shape, dtype=i32, device=self.device) if token is None else token
-        prob = torch.empty(shape, dtype=f32, device=self.device) if prob is None else prob
-        entropy = torch.empty(shape, dtype=f32, device=self.device) if entropy is None else entropy
-        n_kept = torch.empty(shape, dtype=i32, device=self.device) if n_kept is None else n_kept
+        token = u.new_empty(shape, dtype=i32) if token is None else token
+        prob = u.new_empty(shape) if prob is None else prob
+        entropy = u.new_empty(shape) if entropy is None else entropy
+        n_kept = u.new_empty(shape, dtype=i32) if n_kept is None else n_kept
         code = self.lib.sdlm_sample(self.ctx, rows, V, LOGITS_F32 if logits.dtype is f32 else LOGITS_BF16, logits.data_ptr(), stride,
                                     *ins, _is(token, i32, rows, "token"), _is(prob, f32, rows, "prob"),
                                     _is(entropy, f32, rows, "entropy"), _is(n_kept, i32, rows, "n_kept"), _stream_ptr(stream))

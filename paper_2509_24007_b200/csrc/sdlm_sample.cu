@@ -33,7 +33,7 @@
 
 namespace sdlm {
 
-constexpr int kSampleThreads = 512;
+constexpr int kSampleThreads = 256;               // two thread blocks an SM at 128 registers; 512 threads have 64 and spill
 constexpr int kSampleWarps = kSampleThreads / 32;
 constexpr int kSampleBins = 2048;                 // of distance from the maximum: T/102 each, the last one open
 constexpr int kSampleGroups = kSampleBins / 32;   // sums over 32 bins: what thread blocks tell each other first
@@ -118,8 +118,8 @@ struct alignas(16) SampleShared {  // the values behind it are read and written 
   uint64_t group_lo[kSampleGroups], group_hi[kSampleGroups];
   uint32_t lo[2][kSampleSub], hi[2][kSampleSub];  // by parity of the level: one barrier per level then suffices
   uint32_t list[kSampleList];                     // values (bits) of the tokens in question
-  SampleSums mine, extra;                         // what a thread block tells the others of its cluster
-  uint64_t window, below;
+  SampleSums mine, extra[2];                      // what a thread block tells the others of its cluster
+  uint64_t window[2], below[2];
   SampleSums warp[kSampleWarps];
   uint64_t scan[kSampleWarps], scan2[kSampleWarps];
   uint32_t scan32[kSampleWarps];
@@ -128,8 +128,9 @@ struct alignas(16) SampleShared {  // the values behind it are read and written 
   int found, n_list;
   // what the first warp finds in the counts
   int b_k, b0, b1;
-  uint32_t in_k;
   uint64_t before_k;
+  uint32_t sum_n[kSampleGroups], fine_k[32], n_window;  // the cluster's counts by group, of the bins of b_k's group what top-k keeps
+  uint64_t sum_lo[kSampleGroups], sum_hi[kSampleGroups];
 };
 static_assert(sizeof(SampleShared) % 16 == 0, "the values start on a 16-byte boundary");
 
@@ -213,10 +214,10 @@ struct SampleRow {
     }
     return v;
   }
-  // Counts the tokens by bin and finds top-k's bin (b_k, with before_k tokens before it and in_k of it kept) and top-p's
-  // window of bins [b0, b1].  The histograms stay where they are: the thread blocks exchange sums over 32 bins and then only
-  // the bins in question (all of them from all of the others cost more than everything else together).
-  __device__ __forceinline__ void find_bins(bool by_k, int k, bool by_p, double p64) {
+  // Counts the tokens by bin, and finds top-k's bin (b_k, with before_k tokens before it).  The histograms stay where they
+  // are: the thread blocks exchange sums over 32 bins and then only the bins in question (all of them from all of the others
+  // cost more than everything else together).
+  __device__ __forceinline__ void find_bins(bool by_k, int k, bool by_p) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     for (int i = threadIdx.x; i < kSampleBins / 4; i += kSampleThreads) reinterpret_cast<uint4*>(sh->count)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
@@ -257,65 +258,93 @@ struct SampleRow {
         }
       }
       int b_k = kSampleBins;
-      uint32_t in_k = 0, fine_k = 0;
       const uint32_t incl = warp_prefix(n[0] + n[1]), tokens = __shfl_sync(0xffffffffu, incl, 31);
       if (by_k && (uint32_t)k < tokens) {
-        const uint32_t past = __ballot_sync(0xffffffffu, incl >= (uint32_t)k);
-        const int src = __ffs(past) - 1;
+        const int src = __ffs(__ballot_sync(0xffffffffu, incl >= (uint32_t)k)) - 1;
         const uint32_t before = __shfl_sync(0xffffffffu, incl - n[0] - n[1], src), n_0 = __shfl_sync(0xffffffffu, n[0], src);
         const int g = 2 * src + (before + n_0 >= (uint32_t)k ? 0 : 1);
-        const uint32_t first = before + (g & 1 ? n_0 : 0u);
-        fine_k = cluster_bin(g);
-        const uint32_t f_incl = first + warp_prefix(fine_k);
+        uint32_t fine = cluster_bin(g);
+        const uint32_t f_incl = before + (g & 1 ? n_0 : 0u) + warp_prefix(fine);
         const int at = __ffs(__ballot_sync(0xffffffffu, f_incl >= (uint32_t)k)) - 1;
-        const uint32_t before_k = __shfl_sync(0xffffffffu, f_incl - fine_k, at);
+        const uint32_t before_k = __shfl_sync(0xffffffffu, f_incl - fine, at);
         b_k = 32 * g + at;
-        in_k = (uint32_t)k - before_k;
-        fine_k = lane < at ? fine_k : lane == at ? in_k : 0u;  // of that group's bins, what top-k keeps
+        fine = lane < at ? fine : lane == at ? (uint32_t)k - before_k : 0u;
+        sh->fine_k[lane] = fine;
         if (lane == 0) sh->before_k = before_k;
-        if (by_p) {
-          uint64_t l, h;
-          bounds(32 * g + lane, fine_k, l, h);
-          l = sample_warp_sum(l);
-          h = sample_warp_sum(h);
+        // what top-k leaves of the groups
+        uint64_t l, h;
+        bounds(32 * g + lane, fine, l, h);
+        l = sample_warp_sum(l);
+        h = sample_warp_sum(h);
+        const uint32_t m = __reduce_add_sync(0xffffffffu, fine);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            if (2 * lane + i > g) lo[i] = hi[i] = 0;
-            if (2 * lane + i == g) { lo[i] = l; hi[i] = h; }
-          }
+        for (int i = 0; i < 2; ++i) {
+          if (2 * lane + i > g) { n[i] = 0; lo[i] = hi[i] = 0; }
+          if (2 * lane + i == g) { n[i] = m; lo[i] = l; hi[i] = h; }
         }
       }
-      if (lane == 0) {
-        sh->b_k = b_k;
-        sh->in_k = in_k;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        sh->sum_n[2 * lane + i] = n[i];
+        sh->sum_lo[2 * lane + i] = lo[i];
+        sh->sum_hi[2 * lane + i] = hi[i];
       }
-      if (by_p) {
-        // The threshold's bin is one whose weight from above, with all before, can reach top_p of the total (the first such
-        // bin is b0), and none behind the first whose weight from below must reach it (b1).
-        const uint64_t l_incl = warp_prefix(lo[0] + lo[1]), h_incl = warp_prefix(hi[0] + hi[1]);
-        const double goal_lo = p64 * (double)__shfl_sync(0xffffffffu, l_incl, 31) * (1.0 - 1e-12);
-        const double goal_hi = p64 * (double)__shfl_sync(0xffffffffu, h_incl, 31) * (1.0 + 1e-12) + 1.0;
-        auto locate = [&](const uint64_t (&v)[2], uint64_t inclusive, double goal, bool upper) {
-          const uint32_t past = __ballot_sync(0xffffffffu, inclusive > 0 && (double)inclusive >= goal);
-          if (!past) return kSampleBins - 1;
-          const int src = __ffs(past) - 1;
-          const uint64_t before = __shfl_sync(0xffffffffu, inclusive - v[0] - v[1], src), v_0 = __shfl_sync(0xffffffffu, v[0], src);
-          const int g = 2 * src + (before + v_0 > 0 && (double)(before + v_0) >= goal ? 0 : 1);
-          const uint32_t m = g == b_k >> 5 ? fine_k : cluster_bin(g);
-          uint64_t l, h;
-          bounds(32 * g + lane, m, l, h);
-          const uint64_t x = before + (g & 1 ? v_0 : 0) + warp_prefix(upper ? h : l);
-          const uint32_t at = __ballot_sync(0xffffffffu, x > 0 && (double)x >= goal && (!upper || m));
-          return at ? 32 * g + __ffs(at) - 1 : min(32 * g + 31, kSampleBins - 1);
-        };
-        const int b0 = locate(hi, h_incl, goal_lo, true), b1 = locate(lo, l_incl, goal_hi, false);
-        if (lane == 0) {
-          sh->b0 = b0;
-          sh->b1 = min(max(b0, b1), b_k);
-        }
-      }
+      if (lane == 0) sh->b_k = b_k;
     }
     __syncthreads();
+  }
+
+  // The window [b0, b1] of bins that can hold top-p's threshold: the first bin whose weight from above, with all before, can
+  // reach the goal, to the first whose weight from below must.  At first the goal is p of a total that is known between
+  // bounds as well; once the weight before group g0 and of groups [g0, g1] is known (`before`, `mass`, multiples of 2^-45),
+  // it is `want`, and the bounds hold from both ends.  For the first warp; n_window: the tokens of the window.
+  __device__ __forceinline__ void find_window(bool known, int g0, int g1, double before, double mass, double want, double p64) {
+    const int lane = threadIdx.x & 31, g_k = sh->b_k >> 5;
+    uint64_t lo[2], hi[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const bool in = 2 * lane + i >= g0 && 2 * lane + i <= g1;
+      lo[i] = in ? sh->sum_lo[2 * lane + i] : 0;
+      hi[i] = in ? sh->sum_hi[2 * lane + i] : 0;
+    }
+    const uint64_t l_incl = warp_prefix(lo[0] + lo[1]), h_incl = warp_prefix(hi[0] + hi[1]);
+    const double l_all = (double)__shfl_sync(0xffffffffu, l_incl, 31), h_all = (double)__shfl_sync(0xffffffffu, h_incl, 31);
+    const double unit = 1.0 / 32.0, base = known ? before * unit : 0.0, end = base + mass * unit;  // in multiples of 2^-40
+    // weight up to a place with bounds l, h of what lies between the first group and it, from above and from below
+    auto at_most = [&](double l, double h) { return (known ? fmin(base + h, end - (l_all - l)) : h) * (1.0 + 1e-13) + 1.0; };
+    auto at_least = [&](double l, double h) { return (known ? fmax(base + l, end - (h_all - h)) : l) * (1.0 - 1e-13) - 1.0; };
+    auto locate = [&](bool upper) {
+      const double goal = known ? want * unit : upper ? p64 * l_all * (1.0 - 1e-13) : p64 * h_all * (1.0 + 1e-13);
+      const double l1 = (double)l_incl, h1 = (double)h_incl, l0 = (double)(l_incl - lo[1]), h0 = (double)(h_incl - hi[1]);
+      const bool ok0 = (upper ? at_most(l0, h0) : at_least(l0, h0)) >= goal && 2 * lane >= g0;
+      const bool ok1 = (upper ? at_most(l1, h1) : at_least(l1, h1)) >= goal && 2 * lane + 1 >= g0;
+      const uint32_t m0 = __ballot_sync(0xffffffffu, ok0), m1 = __ballot_sync(0xffffffffu, ok1);
+      const int a = m0 ? 2 * (__ffs(m0) - 1) : kSampleGroups, b = m1 ? 2 * (__ffs(m1) - 1) + 1 : kSampleGroups;
+      const int g = min(min(a, b), g1);
+      const uint64_t l_b = __shfl_sync(0xffffffffu, g & 1 ? l_incl - lo[1] : l_incl - lo[0] - lo[1], g >> 1);
+      const uint64_t h_b = __shfl_sync(0xffffffffu, g & 1 ? h_incl - hi[1] : h_incl - hi[0] - hi[1], g >> 1);
+      uint64_t l, h;
+      bounds(32 * g + lane, g == g_k ? sh->fine_k[lane] : cluster_bin(g), l, h);
+      const double lx = (double)(l_b + warp_prefix(l)), hx = (double)(h_b + warp_prefix(h));
+      const uint32_t at = __ballot_sync(0xffffffffu, (upper ? at_most(lx, hx) : at_least(lx, hx)) >= goal);
+      return 32 * g + (at ? __ffs(at) - 1 : 31);
+    };
+    const int b0 = locate(true), b1 = min(max(b0, locate(false)), sh->b_k);
+    // tokens of the window's groups (an upper bound that is near enough)
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) n += 2 * lane + i >= b0 >> 5 && 2 * lane + i <= b1 >> 5 ? sh->sum_n[2 * lane + i] : 0u;
+    if (b0 >> 5 == b1 >> 5 || (b0 >> 5) + 1 == b1 >> 5) {  // few groups: count the bins
+      const int ga = b0 >> 5, gb = b1 >> 5;
+      const uint32_t x = ga == g_k ? sh->fine_k[lane] : cluster_bin(ga), y = gb == ga ? 0u : gb == g_k ? sh->fine_k[lane] : cluster_bin(gb);
+      n = (32 * ga + lane >= b0 && 32 * ga + lane <= b1 ? x : 0u) + (32 * gb + lane <= b1 ? y : 0u);
+    }
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (lane == 0) {
+      sh->b0 = b0;
+      sh->b1 = b1;
+      sh->n_window = n;
+    }
   }
 
   // Lists the tokens of bins [b0, b1] that `floor` keeps whole; n_list is beyond the list's length when they do not fit.
@@ -500,7 +529,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
     const int whole = p.vec ? n / kVec : 0;
     if (F32) {
       const uint32_t* src = static_cast<const uint32_t*>(p.logits) + (long long)row * p.ld + first;
-#pragma unroll 5
+#pragma unroll 8
       for (int i = tid; i < whole; i += kSampleThreads) {
         const uint4 q = __ldg(reinterpret_cast<const uint4*>(src) + i);
         vals[i] = q;
@@ -515,7 +544,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
     } else {
       const uint16_t* src = static_cast<const uint16_t*>(p.logits) + (long long)row * p.ld + first;
       __nv_bfloat162 m2 = __floats2bfloat162_rn(-INFINITY, -INFINITY);
-#pragma unroll 5
+#pragma unroll 8
       for (int i = tid; i < whole; i += kSampleThreads) {
         const uint4 q = __ldg(reinterpret_cast<const uint4*>(src) + i);
         vals[i] = q;
@@ -584,88 +613,115 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
     cut = SampleCut{mx, 1u};
   } else if (mode == 2) {
     const double p64 = fmax((double)top_p, 0.0);
-    s.find_bins(by_k, k, by_p, p64);
-    const int b_k = sh->b_k, b0 = sh->b0, b1 = sh->b1;
+    s.find_bins(by_k, k, by_p);
+    const int b_k = sh->b_k;
     if (b_k < kSampleBins) {
       s.list_bins(b_k, b_k, cut);
       cut = s.template narrow<false>(b_k, b_k, cut, false, sh->before_k, (uint64_t)k);
     }
     if (by_p) {
-      if (tid == 0) sh->n_list = 0;
-      __syncthreads();
       const SampleCut top = cut;
-      // one pass over the weights: above the window, in it (listed), below it
-      uint64_t above = 0, inside = 0, below = 0;
-      double ent = 0.0;
-      uint32_t count = 0;
-      for (int i = tid; i < n_vec; i += kSampleThreads) {
-        float v[kVec];
-        Row::unpack(vals[i], v);
-        float most = v[0];
-#pragma unroll
-        for (int e = 1; e < kVec; ++e) most = fmaxf(most, v[e]);
-        if (!(most > top.value)) continue;
-        uint32_t listed = 0;
-        double d_up = kSampleWhole, d_mid = kSampleWhole, d_low = kSampleWhole;
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const SampleWeight w = s.weight(v[e]);
-          const int b = s.bin_of(v[e]);
-          const bool in = v[e] > top.value, up = in && b < b0, mid = in && !up && b <= b1;
-          const double x = up ? w.w45 : 0.0;
-          d_up += x;
-          ent = fma(x, -w.t, ent);
-          d_mid += mid ? w.w45 : 0.0;
-          d_low += in && !up && !mid ? w.w45 : 0.0;
-          count += up ? 1u : 0u;
-          listed |= mid ? 1u << e : 0u;
-        }
-        above += (uint64_t)__double_as_longlong(d_up) & 0xfffffffffffffull;
-        inside += (uint64_t)__double_as_longlong(d_mid) & 0xfffffffffffffull;
-        below += (uint64_t)__double_as_longlong(d_low) & 0xfffffffffffffull;
-        while (listed) {
-          const int e = __ffs(listed) - 1;
-          listed &= listed - 1;
-          s.put_on_list(Row::pick(v, e));
-        }
-      }
-      above = sample_warp_sum(above);
-      ent = sample_warp_sum(ent);
-      inside = sample_warp_sum(inside);
-      below = sample_warp_sum(below);
-      count = __reduce_add_sync(0xffffffffu, count);
-      if (lane == 0) {
-        sh->warp[warp] = SampleSums{above, ent, count, 0u};
-        sh->scan[warp] = inside;
-        sh->scan2[warp] = below;
-      }
-      __syncthreads();
-      if (tid == 0) {
-        SampleSums a{0, 0.0, 0, 0};
-        uint64_t w_in = 0, w_be = 0;
-        for (int i = 0; i < kSampleWarps; ++i) {
-          a.mass += sh->warp[i].mass;
-          a.ent += sh->warp[i].ent;
-          a.count += sh->warp[i].count;
-          w_in += sh->scan[i];
-          w_be += sh->scan2[i];
-        }
-        sh->extra = a;
-        sh->window = w_in;
-        sh->below = w_be;
-      }
-      ptx::cluster_sync_all();
-      uint64_t all_above = 0, all = 0;
-      for (uint32_t r = 0; r < C; ++r) {
-        const uint64_t a = ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->extra.mass), r));
-        all_above += a;
-        all += a + ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->window), r)) +
-               ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->below), r));
-      }
       const bool tied_k = b_k < kSampleBins;  // top-k kept some of the tokens that equal its threshold (they are not listed)
-      if (tied_k) all += sample_whole(s.weight(top.value).w45) * top.take;
-      const double goal = ceil(p64 * (double)all);
-      const uint64_t want = goal >= (double)all ? all : goal < 1.0 ? 1 : (uint64_t)goal;
+      const uint64_t tied = tied_k ? sample_whole(s.weight(top.value).w45) * top.take : 0;
+      int b0, b1, from = 0, upto = kSampleBins - 1;
+      uint64_t all_above = 0, all = 0, want = 0, in_window = 0;
+      own = SampleSums{0, 0.0, 0, 0};
+      for (int pass = 0; pass < 2; ++pass) {
+        if (warp == 0) s.find_window(pass > 0, from >> 5, upto >> 5, (double)all_above, (double)in_window, (double)want, p64);
+        if (tid == 0) sh->n_list = 0;
+        __syncthreads();
+        b0 = sh->b0;
+        b1 = sh->b1;
+        // many tokens (a wide window in a thin tail): no list yet, but whole groups, and a second look with the sums known
+        const bool wide = pass == 0 && sh->n_window > (uint32_t)(kSampleList / 2) * C;
+        if (wide) {
+          b0 &= ~31;
+          b1 |= 31;
+        }
+        // one pass over the weights of bins [from, upto]: above the window, in it (listed), below it
+        uint64_t above = 0, inside = 0, below = 0;
+        double ent = 0.0;
+        uint32_t count = 0;
+        for (int i = tid; i < n_vec; i += kSampleThreads) {
+          float v[kVec];
+          Row::unpack(vals[i], v);
+          uint32_t some = 0;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) {
+            const int b = s.bin_of(v[e]);
+            some |= v[e] > top.value && b >= from && b <= upto ? 1u << e : 0u;
+          }
+          if (!some) continue;
+          uint32_t listed = 0;
+          double d_up = kSampleWhole, d_mid = kSampleWhole, d_low = kSampleWhole;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) {
+            const SampleWeight w = s.weight(v[e]);
+            const int b = s.bin_of(v[e]);
+            const bool in = some >> e & 1u, up = in && b < b0, mid = in && !up && b <= b1;
+            const double x = up ? w.w45 : 0.0;
+            d_up += x;
+            ent = fma(x, -w.t, ent);
+            d_mid += mid ? w.w45 : 0.0;
+            d_low += in && !up && !mid ? w.w45 : 0.0;
+            count += up ? 1u : 0u;
+            listed |= mid ? 1u << e : 0u;
+          }
+          above += (uint64_t)__double_as_longlong(d_up) & 0xfffffffffffffull;
+          inside += (uint64_t)__double_as_longlong(d_mid) & 0xfffffffffffffull;
+          below += (uint64_t)__double_as_longlong(d_low) & 0xfffffffffffffull;
+          while (listed && !wide) {
+            const int e = __ffs(listed) - 1;
+            listed &= listed - 1;
+            s.put_on_list(Row::pick(v, e));
+          }
+        }
+        above = sample_warp_sum(above);
+        ent = sample_warp_sum(ent);
+        inside = sample_warp_sum(inside);
+        below = sample_warp_sum(below);
+        count = __reduce_add_sync(0xffffffffu, count);
+        if (lane == 0) {
+          sh->warp[warp] = SampleSums{above, ent, count, 0u};
+          sh->scan[warp] = inside;
+          sh->scan2[warp] = below;
+        }
+        __syncthreads();
+        if (tid == 0) {
+          SampleSums a{0, 0.0, 0, 0};
+          uint64_t w_in = 0, w_be = 0;
+          for (int i = 0; i < kSampleWarps; ++i) {
+            a.mass += sh->warp[i].mass;
+            a.ent += sh->warp[i].ent;
+            a.count += sh->warp[i].count;
+            w_in += sh->scan[i];
+            w_be += sh->scan2[i];
+          }
+          sh->extra[pass] = a;
+          sh->window[pass] = w_in;
+          sh->below[pass] = w_be;
+        }
+        ptx::cluster_sync_all();
+        in_window = 0;
+        uint64_t rest = 0;
+        for (uint32_t r = 0; r < C; ++r) {
+          all_above += ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->extra[pass].mass), r));
+          in_window += ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->window[pass]), r));
+          rest += ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->below[pass]), r));
+        }
+        own.mass += sh->extra[pass].mass;
+        own.ent += sh->extra[pass].ent;
+        own.count += sh->extra[pass].count;
+        if (pass == 0) {
+          all = all_above + in_window + rest + tied;
+          const double goal = ceil(p64 * (double)all);
+          want = goal >= (double)all ? all : goal < 1.0 ? 1 : (uint64_t)goal;
+          if (tied_k && b_k <= b1) in_window += tied;  // (b_k is in the window then, as the window ends there at the latest)
+        }
+        if (!wide) break;
+        from = b0;
+        upto = b1;
+      }
       cut = s.template narrow<true>(b0, b1, top, tied_k && b_k <= b1, all_above, want);
       if (tied_k && cut.value == top.value) cut.take = min(cut.take, top.take);
       // this thread block's kept tokens: those above the window and the listed ones above the cut
@@ -695,7 +751,6 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
       t2 = __reduce_add_sync(0xffffffffu, t2);
       if (lane == 0) sh->warp[warp] = SampleSums{m2, 4.0 * (double)e2, c2, t2};  // (the sums over the list in whole numbers)
       __syncthreads();
-      own = sh->extra;
 #pragma unroll 1
       for (int i = 0; i < kSampleWarps; ++i) {
         own.mass += sh->warp[i].mass;

@@ -29,7 +29,7 @@ namespace sdlm {
 constexpr int kTreeThreads = 384;
 constexpr int kTreeRows = 256;        // stacked rows of a task
 constexpr float kTreeRebase = 8.0f;   // log2 units a score may exceed its row's reference by
-constexpr int kTreeItemCost = 4;      // key tiles' worth of work the schedule charges for a task's queries and output
+constexpr int kTreeItemCost = 8;      // key tiles' worth of work the schedule charges for a task's queries and output
 constexpr int kTreeSmemLimit = 232448;
 
 struct TreeParams {
