@@ -31,6 +31,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace sdlm {
 
 constexpr int kSampleThreads = 256;               // two thread blocks an SM at 128 registers; 512 threads have 64 and spill
@@ -40,6 +42,7 @@ constexpr int kSampleGroups = kSampleBins / 32;   // sums over 32 bins: what thr
 constexpr int kSampleSub = 128;                   // parts a key range is cut into
 constexpr int kSampleList = 2048;                 // tokens of a bin or window that a thread block lists
 constexpr int kSampleMaxVocab = 1 << 18;
+constexpr uint32_t kSampleCluster = 8;            // thread blocks of a row, at most (the portable cluster size)
 
 struct SampleParams {
   const void* logits;
@@ -69,12 +72,16 @@ __device__ __forceinline__ float sample_value(uint32_t key) {
   return __uint_as_float((key & 0x8000u ? key ^ 0x8000u : ~key & 0xffffu) << 16);
 }
 
-// Weight of a value: t = z log2 e (0 at the maximum; -200 below v_floor, and 2^-200 adds nothing) and w = 2^t, with a relative
-// error below 6e-12, as a whole multiple of 2^-45, in a double.
+// Weight of a value: t = z log2 e (0 at the maximum; -200 below v_floor, and 2^-200 adds nothing) and w45 = 2^t 2^45 with a
+// relative error below 6e-12; `whole` is that as a whole number (64-bit integers add up beside the pipe of the doubles).
 struct SampleWeight {
   double t, w45;
+  uint64_t whole;
 };
 constexpr double kSampleWhole = 4503599627370496.0;  // 2^52: adding it leaves the nearest whole number in the mantissa
+__device__ __forceinline__ uint64_t sample_whole(double x) {  // a number below 2^52, to the nearest whole one
+  return (uint64_t)__double_as_longlong(x + kSampleWhole) & 0xfffffffffffffull;
+}
 __device__ __forceinline__ SampleWeight sample_weight(float v, float v_floor, double vmax, double scale) {
   SampleWeight r;
   r.t = v >= v_floor ? ((double)v - vmax) * scale : -200.0;  // (a NaN is not)
@@ -89,15 +96,12 @@ __device__ __forceinline__ SampleWeight sample_weight(float v, float v_floor, do
   q = fma(q, f, 2.4022650695910071e-01);
   q = fma(q, f, 6.9314718055994531e-01);
   q = fma(q, f, 1.0);
-  const double w45 = __hiloint2double(__double2hiint(q) + ((__double2loint(m) + 45) << 20), __double2loint(q));
-  r.w45 = (w45 + kSampleWhole) - kSampleWhole;     // at most 2^45
+  r.w45 = __hiloint2double(__double2hiint(q) + ((__double2loint(m) + 45) << 20), __double2loint(q));  // at most 2^45
+  r.whole = sample_whole(r.w45);
   return r;
 }
-__device__ __forceinline__ uint64_t sample_whole(double x) {  // a whole number below 2^52
-  return (uint64_t)__double_as_longlong(x + kSampleWhole) & 0xfffffffffffffull;
-}
 // -w t as a multiple of 2^-43 (w |t| <= 0.54), for sums whose order is not fixed.
-__device__ __forceinline__ uint64_t sample_entropy(const SampleWeight& w) { return sample_whole(rint(w.w45 * w.t * -0.25)); }
+__device__ __forceinline__ uint64_t sample_entropy(const SampleWeight& w) { return sample_whole(w.w45 * w.t * -0.25); }
 
 // Tokens above `value` are kept, and the first `take` by index of those that equal it.
 struct SampleCut {
@@ -119,12 +123,12 @@ struct alignas(16) SampleShared {  // the values behind it are read and written 
   uint32_t lo[2][kSampleSub], hi[2][kSampleSub];  // by parity of the level: one barrier per level then suffices
   uint32_t list[kSampleList];                     // values (bits) of the tokens in question
   SampleSums mine, extra[2];                      // what a thread block tells the others of its cluster
-  uint64_t window[2], below[2];
+  uint64_t window[2], looked[2];
   SampleSums warp[kSampleWarps];
   uint64_t scan[kSampleWarps], scan2[kSampleWarps];
   uint32_t scan32[kSampleWarps];
   uint64_t found_before;
-  float max_value;
+  uint32_t max_bits;
   int found, n_list;
   // what the first warp finds in the counts
   int b_k, b0, b1;
@@ -160,6 +164,30 @@ __device__ __forceinline__ N sample_warp_sum(N v) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
+}
+
+// What the C thread blocks of a cluster have at the same place, loads in flight together (a loop over C waits for each).
+template <typename N>
+__device__ __forceinline__ void sample_gather(const N* at, uint32_t C, N (&v)[kSampleCluster]) {
+  static_assert(sizeof(N) == 4 || sizeof(N) == 8, "");
+  const uint32_t a = ptx::smem_u32(at);
+#pragma unroll
+  for (uint32_t r = 0; r < kSampleCluster; ++r) {
+    v[r] = 0;
+    if (r < C) {
+      if constexpr (sizeof(N) == 4) v[r] = (N)ptx::ld_cluster_u32(ptx::mapa_u32(a, r));
+      else if constexpr (std::is_same<N, double>::value) v[r] = __longlong_as_double((long long)ptx::ld_cluster_u64(ptx::mapa_u32(a, r)));
+      else v[r] = (N)ptx::ld_cluster_u64(ptx::mapa_u32(a, r));
+    }
+  }
+}
+template <typename N>
+__device__ __forceinline__ N sample_cluster_sum(const N* at, uint32_t C) {
+  N v[kSampleCluster];
+  sample_gather(at, C, v);
+#pragma unroll
+  for (uint32_t r = 1; r < kSampleCluster; ++r) v[0] += v[r];
+  return v[0];
 }
 
 template <bool F32>
@@ -201,9 +229,7 @@ struct SampleRow {
   }
   // Tokens of bin 32 g + lane in the whole cluster; whole warps.
   __device__ __forceinline__ uint32_t cluster_bin(int g) const {
-    uint32_t n = 0;
-    for (int r = 0; r < C; ++r) n += ptx::ld_cluster_u32(ptx::mapa_u32(ptx::smem_u32(&sh->count[32 * g + (threadIdx.x & 31)]), r));
-    return n;
+    return sample_cluster_sum(&sh->count[32 * g + (threadIdx.x & 31)], C);
   }
   template <typename N>
   static __device__ __forceinline__ N warp_prefix(N v) {  // inclusive
@@ -247,14 +273,12 @@ struct SampleRow {
       static_assert(kSampleGroups == 64, "two groups a lane");
       uint32_t n[2] = {0, 0};
       uint64_t lo[2] = {0, 0}, hi[2] = {0, 0};
-      for (int r = 0; r < C; ++r) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          n[i] += ptx::ld_cluster_u32(ptx::mapa_u32(ptx::smem_u32(&sh->group_n[2 * lane + i]), r));
-          if (by_p) {
-            lo[i] += ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->group_lo[2 * lane + i]), r));
-            hi[i] += ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->group_hi[2 * lane + i]), r));
-          }
+      for (int i = 0; i < 2; ++i) {
+        n[i] = sample_cluster_sum(&sh->group_n[2 * lane + i], C);
+        if (by_p) {
+          lo[i] = sample_cluster_sum(&sh->group_lo[2 * lane + i], C);
+          hi[i] = sample_cluster_sum(&sh->group_hi[2 * lane + i], C);
         }
       }
       int b_k = kSampleBins;
@@ -367,17 +391,15 @@ struct SampleRow {
       while (in) {
         const int e = __ffs(in) - 1;
         in &= in - 1;
-        put_on_list(pick(v, e));
+        put_on_list(at(i * kVec + e));
       }
     }
     __syncthreads();
   }
-  // v[e] without an array in local memory
-  static __device__ __forceinline__ float pick(const float (&v)[kVec], int e) {
-    float x = v[0];
-#pragma unroll
-    for (int i = 1; i < kVec; ++i) x = e == i ? v[i] : x;
-    return x;
+  // The slice's value at a place known only at run time (indexing the registers it was unpacked to would put them in memory).
+  __device__ __forceinline__ float at(int i) const {
+    if (F32) return reinterpret_cast<const float*>(vals)[i];
+    return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(vals)[i] << 16);
   }
   // f(value) for the tokens listed (of bins [b0, b1] above the floor), from the slice when the list was too short.
   template <typename F>
@@ -388,12 +410,13 @@ struct SampleRow {
       for (int i = threadIdx.x; i < n_vec; i += kSampleThreads) {
         float v[kVec];
         unpack(vals[i], v);
-#pragma unroll 1
-        for (int e = 0; e < kVec; ++e)
-          if (v[e] > floor.value) {
-            const int b = bin_of(v[e]);
-            if (b >= b0 && b <= b1) f(v[e]);
-          }
+        uint32_t in = 0;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+          const int b = bin_of(v[e]);
+          in |= v[e] > floor.value && b >= b0 && b <= b1 ? 1u << e : 0u;
+        }
+        for (; in; in &= in - 1) f(at(i * kVec + __ffs(in) - 1));
       }
     }
   }
@@ -428,7 +451,7 @@ struct SampleRow {
         if (key < r_lo || key > r_hi) return;
         const uint32_t i = (r_hi - key) >> part;
         if (MASS) {
-          const uint64_t w = sample_whole(weight(v).w45) * n;
+          const uint64_t w = weight(v).whole * n;
           // 64 bits in two halves; the carry goes with whoever brought the lower half over
           const uint32_t w_lo = (uint32_t)w, old = atomicAdd(&lo[i], w_lo);
           const uint32_t up = (uint32_t)(w >> 32) + (old + w_lo < old ? 1u : 0u);
@@ -442,10 +465,11 @@ struct SampleRow {
       ptx::cluster_sync_all();
       uint64_t v = 0;
       if (threadIdx.x < kSampleSub) {
-        for (int r = 0; r < C; ++r) {
-          v += ptx::ld_cluster_u32(ptx::mapa_u32(ptx::smem_u32(&lo[threadIdx.x]), r));
-          if (MASS) v += (uint64_t)ptx::ld_cluster_u32(ptx::mapa_u32(ptx::smem_u32(&hi[threadIdx.x]), r)) << 32;
-        }
+        uint32_t a[kSampleCluster], b[kSampleCluster] = {};
+        sample_gather(&lo[threadIdx.x], C, a);
+        if (MASS) sample_gather(&hi[threadIdx.x], C, b);
+#pragma unroll
+        for (uint32_t r = 0; r < kSampleCluster; ++r) v += (uint64_t)a[r] + ((uint64_t)b[r] << 32);
       }
       uint64_t total;
       const uint64_t e = before + sample_scan(v, sh->scan, total);
@@ -462,7 +486,7 @@ struct SampleRow {
       if (r_hi == r_lo) break;
     }
     const float value = sample_value<F32>(r_hi);
-    const uint64_t each = MASS ? max((uint64_t)1, sample_whole(weight(value).w45)) : 1;
+    const uint64_t each = MASS ? max((uint64_t)1, weight(value).whole) : 1;
     return SampleCut{value, (uint32_t)((want - before + each - 1) / each)};
   }
 
@@ -479,18 +503,15 @@ struct SampleRow {
       for (int e = 1; e < kVec; ++e) mx = fmaxf(mx, v[e]);
       if (!(mx >= reject)) continue;
       // (no branch on a single token: eight chains of 64-bit operations at a time keep their pipe fed, one does not)
-      double sum = kSampleWhole;  // whole numbers, below 2^48 together
 #pragma unroll
       for (int e = 0; e < kVec; ++e) {
         const SampleWeight w = weight(v[e]);
         const bool in = v[e] > cut.value && v[e] >= reject && w.t >= min_t;
-        const double x = in ? w.w45 : 0.0;
-        sum += x;
-        s.ent = fma(x, -w.t, s.ent);
+        s.mass += in ? w.whole : 0;
+        s.ent = fma(in ? w.w45 : 0.0, -w.t, s.ent);
         s.count += in ? 1u : 0u;
         s.ties += v[e] == cut.value && v[e] > -INFINITY ? 1u : 0u;
       }
-      s.mass += (uint64_t)__double_as_longlong(sum) & 0xfffffffffffffull;
     }
     s.mass = sample_warp_sum(s.mass);
     s.ent = sample_warp_sum(s.ent);
@@ -566,9 +587,14 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kSampleWarps; ++i) mx = fmaxf(mx, __uint_as_float(sh->scan32[i]));
-  if (tid == 0) sh->max_value = mx;
+  if (tid == 0) sh->max_bits = __float_as_uint(mx);
   ptx::cluster_sync_all();
-  for (uint32_t r = 0; r < C; ++r) mx = fmaxf(mx, __uint_as_float(ptx::ld_cluster_u32(ptx::mapa_u32(ptx::smem_u32(&sh->max_value), r))));
+  {
+    uint32_t all[kSampleCluster];
+    sample_gather(&sh->max_bits, C, all);
+#pragma unroll
+    for (uint32_t r = 0; r < kSampleCluster; ++r) mx = r < C ? fmaxf(mx, __uint_as_float(all[r])) : mx;
+  }
   if (!(mx > -INFINITY)) {  // no token can be taken
     if (rank == 0 && tid == 0) {
       p.token[row] = -1;
@@ -622,9 +648,9 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
     if (by_p) {
       const SampleCut top = cut;
       const bool tied_k = b_k < kSampleBins;  // top-k kept some of the tokens that equal its threshold (they are not listed)
-      const uint64_t tied = tied_k ? sample_whole(s.weight(top.value).w45) * top.take : 0;
+      const uint64_t tied = tied_k ? s.weight(top.value).whole * top.take : 0;
       int b0, b1, from = 0, upto = kSampleBins - 1;
-      uint64_t all_above = 0, all = 0, want = 0, in_window = 0;
+      uint64_t all_above = 0, want = 0, in_window = 0;
       own = SampleSums{0, 0.0, 0, 0};
       for (int pass = 0; pass < 2; ++pass) {
         if (warp == 0) s.find_window(pass > 0, from >> 5, upto >> 5, (double)all_above, (double)in_window, (double)want, p64);
@@ -639,81 +665,97 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
           b1 |= 31;
         }
         // one pass over the weights of bins [from, upto]: above the window, in it (listed), below it
-        uint64_t above = 0, inside = 0, below = 0;
+        uint64_t above = 0, inside = 0, all_mine = 0;
         double ent = 0.0;
         uint32_t count = 0;
-        for (int i = tid; i < n_vec; i += kSampleThreads) {
-          float v[kVec];
-          Row::unpack(vals[i], v);
-          uint32_t some = 0;
+        if (pass == 0 && !tied_k) {  // every token counts: eight chains of 64-bit operations at a time keep their pipe fed
+          for (int i = tid; i < n_vec; i += kSampleThreads) {
+            float v[kVec];
+            Row::unpack(vals[i], v);
+            uint32_t listed = 0;
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) {
-            const int b = s.bin_of(v[e]);
-            some |= v[e] > top.value && b >= from && b <= upto ? 1u << e : 0u;
+            for (int e = 0; e < kVec; ++e) {
+              const SampleWeight w = s.weight(v[e]);  // (0 for -inf and NaN)
+              const int b = s.bin_of(v[e]);
+              const bool up = b < b0, mid = !up && b <= b1;
+              all_mine += w.whole;
+              above += up ? w.whole : 0;
+              inside += mid ? w.whole : 0;
+              ent = fma(up ? w.w45 : 0.0, -w.t, ent);
+              count += up && v[e] > -INFINITY ? 1u : 0u;
+              listed |= mid && v[e] > -INFINITY ? 1u << e : 0u;
+            }
+            while (listed && !wide) {
+              const int e = __ffs(listed) - 1;
+              listed &= listed - 1;
+              s.put_on_list(s.at(i * kVec + e));
+            }
           }
-          if (!some) continue;
-          uint32_t listed = 0;
-          double d_up = kSampleWhole, d_mid = kSampleWhole, d_low = kSampleWhole;
+        } else {
+          for (int i = tid; i < n_vec; i += kSampleThreads) {
+            float v[kVec];
+            Row::unpack(vals[i], v);
+            uint32_t some = 0;
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) {
-            const SampleWeight w = s.weight(v[e]);
-            const int b = s.bin_of(v[e]);
-            const bool in = some >> e & 1u, up = in && b < b0, mid = in && !up && b <= b1;
-            const double x = up ? w.w45 : 0.0;
-            d_up += x;
-            ent = fma(x, -w.t, ent);
-            d_mid += mid ? w.w45 : 0.0;
-            d_low += in && !up && !mid ? w.w45 : 0.0;
-            count += up ? 1u : 0u;
-            listed |= mid ? 1u << e : 0u;
-          }
-          above += (uint64_t)__double_as_longlong(d_up) & 0xfffffffffffffull;
-          inside += (uint64_t)__double_as_longlong(d_mid) & 0xfffffffffffffull;
-          below += (uint64_t)__double_as_longlong(d_low) & 0xfffffffffffffull;
-          while (listed && !wide) {
-            const int e = __ffs(listed) - 1;
-            listed &= listed - 1;
-            s.put_on_list(Row::pick(v, e));
+            for (int e = 0; e < kVec; ++e) {
+              const int b = s.bin_of(v[e]);
+              some |= v[e] > top.value && b >= from && b <= upto ? 1u << e : 0u;
+            }
+            if (!some) continue;  // (a weight at a time for those of them took a quarter longer than all of them side by side)
+            uint32_t listed = 0;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+              const SampleWeight w = s.weight(v[e]);
+              const int b = s.bin_of(v[e]);
+              const bool in = some >> e & 1u, up = in && b < b0, mid = in && !up && b <= b1;
+              all_mine += in ? w.whole : 0;
+              above += up ? w.whole : 0;
+              inside += mid ? w.whole : 0;
+              ent = fma(up ? w.w45 : 0.0, -w.t, ent);
+              count += up ? 1u : 0u;
+              listed |= mid ? 1u << e : 0u;
+            }
+            while (listed && !wide) {
+              const int e = __ffs(listed) - 1;
+              listed &= listed - 1;
+              s.put_on_list(s.at(i * kVec + e));
+            }
           }
         }
         above = sample_warp_sum(above);
         ent = sample_warp_sum(ent);
         inside = sample_warp_sum(inside);
-        below = sample_warp_sum(below);
+        all_mine = sample_warp_sum(all_mine);
         count = __reduce_add_sync(0xffffffffu, count);
         if (lane == 0) {
           sh->warp[warp] = SampleSums{above, ent, count, 0u};
           sh->scan[warp] = inside;
-          sh->scan2[warp] = below;
+          sh->scan2[warp] = all_mine;
         }
         __syncthreads();
         if (tid == 0) {
           SampleSums a{0, 0.0, 0, 0};
-          uint64_t w_in = 0, w_be = 0;
+          uint64_t w_in = 0, w_all = 0;
           for (int i = 0; i < kSampleWarps; ++i) {
             a.mass += sh->warp[i].mass;
             a.ent += sh->warp[i].ent;
             a.count += sh->warp[i].count;
             w_in += sh->scan[i];
-            w_be += sh->scan2[i];
+            w_all += sh->scan2[i];
           }
           sh->extra[pass] = a;
           sh->window[pass] = w_in;
-          sh->below[pass] = w_be;
+          sh->looked[pass] = w_all;
         }
         ptx::cluster_sync_all();
-        in_window = 0;
-        uint64_t rest = 0;
-        for (uint32_t r = 0; r < C; ++r) {
-          all_above += ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->extra[pass].mass), r));
-          in_window += ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->window[pass]), r));
-          rest += ptx::ld_cluster_u64(ptx::mapa_u32(ptx::smem_u32(&sh->below[pass]), r));
-        }
+        all_above += sample_cluster_sum(&sh->extra[pass].mass, C);
+        in_window = sample_cluster_sum(&sh->window[pass], C);
+        
         own.mass += sh->extra[pass].mass;
         own.ent += sh->extra[pass].ent;
         own.count += sh->extra[pass].count;
         if (pass == 0) {
-          all = all_above + in_window + rest + tied;
+          const uint64_t all = sample_cluster_sum(&sh->looked[pass], C) + tied;
           const double goal = ceil(p64 * (double)all);
           want = goal >= (double)all ? all : goal < 1.0 ? 1 : (uint64_t)goal;
           if (tied_k && b_k <= b1) in_window += tied;  // (b_k is in the window then, as the window ends there at the latest)
@@ -730,7 +772,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
       s.each_listed(b0, b1, top, [&](float v) {
         if (v > cut.value) {
           const SampleWeight w = s.weight(v);
-          m2 += sample_whole(w.w45);
+          m2 += w.whole;
           e2 += sample_entropy(w);
           ++c2;
         } else if (v == cut.value) {
@@ -793,16 +835,22 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
   ptx::cluster_sync_all();
   const bool has_cut = cut.value > -INFINITY;
   const SampleWeight tie = s.weight(has_cut ? cut.value : mx);
-  const uint64_t tie_fix = has_cut ? sample_whole(tie.w45) : 0;
+  const uint64_t tie_fix = has_cut ? tie.whole : 0;
   uint32_t take = has_cut && tie.t >= min_t ? cut.take : 0u;
   uint64_t W = 0, my_first = 0, my_mass = 0;
   double sum_ent = 0.0;
   uint32_t my_take = 0, kept = 0;
-  for (uint32_t r = 0; r < C; ++r) {
-    const uint32_t a = ptx::mapa_u32(ptx::smem_u32(&sh->mine), r);
-    const uint64_t m = ptx::ld_cluster_u64(a + offsetof(SampleSums, mass));
-    const uint32_t t = min(take, ptx::ld_cluster_u32(a + offsetof(SampleSums, ties)));
-    const uint64_t all = m + (uint64_t)t * tie_fix;
+  uint64_t masses[kSampleCluster];
+  double ents[kSampleCluster];
+  uint32_t counts[kSampleCluster], tied[kSampleCluster];
+  sample_gather(&sh->mine.mass, C, masses);
+  sample_gather(&sh->mine.ent, C, ents);
+  sample_gather(&sh->mine.count, C, counts);
+  sample_gather(&sh->mine.ties, C, tied);
+#pragma unroll
+  for (uint32_t r = 0; r < kSampleCluster; ++r) {  // (zeros from C on)
+    const uint32_t t = min(take, tied[r]);
+    const uint64_t all = masses[r] + (uint64_t)t * tie_fix;
     if (r == rank) {
       my_first = W;
       my_mass = all;
@@ -810,8 +858,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
     }
     W += all;
     take -= t;
-    kept += ptx::ld_cluster_u32(a + offsetof(SampleSums, count)) + t;
-    sum_ent += __longlong_as_double((long long)ptx::ld_cluster_u64(a + offsetof(SampleSums, ent)));
+    kept += counts[r] + t;
+    sum_ent += ents[r];
     if (has_cut) sum_ent = fma((double)t, -tie.w45 * tie.t, sum_ent);
   }
   ptx::cluster_sync_all();  // nothing of another thread block is read after this
@@ -852,7 +900,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
       const SampleWeight x = s.weight(v[e]);
-      m[e] = v[e] > cut.value && x.t >= min_t ? sample_whole(x.w45) : 0;
+      m[e] = v[e] > cut.value && x.t >= min_t ? x.whole : 0;
       ties += v[e] == cut.value && has_cut ? 1u : 0u;
       mass += m[e];
     }
