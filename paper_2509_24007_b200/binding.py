@@ -8,6 +8,7 @@ CUDA device, creating a context raises -- there is no fallback path.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional, Sequence, Tuple
@@ -64,17 +65,24 @@ def accept_commit_layers(contexts, tau: float, token, p_top1, entropy, k_blks, v
 def tree_commit_layers(contexts, draft_token, next_token, parent, k_trees, v_trees, n_nodes=None, accepted_len=None,
                        out_tokens=None, path=None, seq_ids=None, stream=None):
     """sdlm_tree_commit_layers: one pass over the trees commits the accepted paths into every layer's cache."""
+    if stream is not None:  # the outputs made here are allocated on it too
+        with torch.cuda.stream(stream):
+            return tree_commit_layers(contexts, draft_token, next_token, parent, k_trees, v_trees, n_nodes, accepted_len,
+                                      out_tokens, path, seq_ids)
     sd0 = contexts[0]
     n_layers = len(contexts)
     if len(k_trees) != n_layers or len(v_trees) != n_layers:
         raise ValueError("k_trees and v_trees must hold one tensor per context")
+    for t in (draft_token, next_token, parent, n_nodes, accepted_len, out_tokens, path, seq_ids, *k_trees, *v_trees):
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != sd0.device_index:
+            raise ValueError(f"a tensor is on GPU {t.get_device()}, the contexts on GPU {sd0.device_index}")
     before, after, outs = sd0._tree_commit_args(parent, n_nodes, seq_ids, draft_token, next_token, accepted_len, out_tokens, path)
     rows = (*parent.shape, sd0.cfg.n_kv_heads, sd0.cfg.head_dim)
     ctx_arr = (C.c_void_p * n_layers)(*[c.ctx.value for c in contexts])
     k_arr = (C.c_void_p * n_layers)(*[_shaped(t, torch.bfloat16, rows, "k_tree") for t in k_trees])
     v_arr = (C.c_void_p * n_layers)(*[_shaped(t, torch.bfloat16, rows, "v_tree") for t in v_trees])
     sd0._check("sdlm_tree_commit_layers", sd0.lib.sdlm_tree_commit_layers(
-        ctx_arr, n_layers, *parent.shape, *before, k_arr, v_arr, *after, _stream_ptr(stream)))
+        ctx_arr, n_layers, *parent.shape, *before, k_arr, v_arr, *after, _stream_ptr(None)))
     return outs
 
 
@@ -303,6 +311,25 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
     return (stream or torch.cuda.current_stream()).cuda_stream
 
 
+def _placed(call):
+    """For calls that make their outputs: with `stream` the call runs with that stream current, so that the outputs are
+    allocated (and cleared) on it too; tensors of another GPU than the context's are refused."""
+    @functools.wraps(call)
+    def placed(self, *args, stream=None, **kw):
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return placed(self, *args, **kw)
+        index = self.device_index
+        for t in args:
+            if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != index:
+                raise ValueError(f"a tensor is on GPU {t.get_device()}, the context on GPU {index}")
+        for name, t in kw.items():
+            if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != index:
+                raise ValueError(f"{name} is on GPU {t.get_device()}, the context on GPU {index}")
+        return call(self, *args, **kw)
+    return placed
+
+
 def _is(t, dtype, numel: int, name: str) -> int:
     """Address of a contiguous CUDA tensor of `numel` elements of dtype; None stays None."""
     if t is None:
@@ -332,6 +359,7 @@ class Sdlm:
             raise SdlmError("sdlm_create", 5, "no CUDA device: the library has no CPU path")
         self.cfg = cfg
         self.device = torch.device("cuda", torch.cuda.current_device() if device is None else device)
+        self.device_index = self.device.index
         c = cfg.to_c()
         pool_bytes = self.lib.sdlm_pool_bytes(C.byref(c))
         ws_bytes = self.lib.sdlm_workspace_bytes(C.byref(c))
@@ -720,12 +748,13 @@ class Sdlm:
                                                         _ptr(_dev(out, torch.bfloat16, "out")), _stream_ptr(stream)))
         return out
 
-    # ---- verification of a drafted tree, sampling ----------------------------------------
+    # ---- verification of a drafted tree, sampling (all take stream= as well: _placed) ------
+    @_placed
     def qk_norm_rope(self, q: torch.Tensor, k: Optional[torch.Tensor], rope: RopeConfig,
                      positions: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
                      k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, relative: bool = False,
                      q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
-                     seq_ids: Optional[torch.Tensor] = None, stream=None):
+                     seq_ids: Optional[torch.Tensor] = None):
         """sdlm_qk_norm_rope: q [batch, D, n_heads, d] and k [batch, D, n_heads2, d] or None; either may be a slice of
         the heads of a wider tensor (a stacked q/k/v product)."""
         d = self.cfg.head_dim
@@ -747,7 +776,7 @@ class Sdlm:
             self.ctx, batch, D, _is(seq_ids, torch.int32, batch, "seq_ids"), _is(positions, torch.int32, batch * D, "positions"),
             1 if relative else 0, C.byref(rope.to_c()), eps, heads, q.data_ptr(), q_stride,
             _is(q_weight, torch.bfloat16, d, "q_weight"), _shaped(q_out, torch.bfloat16, q.shape, "q_out"), heads2, k_ptr, k_stride,
-            _is(k_weight, torch.bfloat16, d, "k_weight"), k_out_ptr, _stream_ptr(stream))
+            _is(k_weight, torch.bfloat16, d, "k_weight"), k_out_ptr, _stream_ptr(None))
         if code:
             self._check("sdlm_qk_norm_rope", code)
         return q_out, k_out
@@ -758,9 +787,10 @@ class Sdlm:
             raise ValueError("parent must be [batch, n]")
         return parent.shape
 
+    @_placed
     def tree_attn(self, q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor, parent: torch.Tensor,
                   n_nodes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
-                  seq_ids: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+                  seq_ids: Optional[torch.Tensor] = None) -> torch.Tensor:
         """sdlm_tree_attn: q [batch, n, Hq, d], k_tree / v_tree [batch, n, Hkv, d], parent [batch, n] int32.  Rows of
         `out` behind a sequence's nodes are left as they are (zero when `out` is made here)."""
         if out is None:
@@ -772,7 +802,7 @@ class Sdlm:
             self.ctx, batch, n, _is(seq_ids, torch.int32, batch, "seq_ids"), _is(n_nodes, torch.int32, batch, "n_nodes"),
             _shaped(parent, torch.int32, (batch, n), "parent"), _shaped(q, bf16, rows, "q"),
             _shaped(k_tree, bf16, kv_rows, "k_tree"), _shaped(v_tree, bf16, kv_rows, "v_tree"), _shaped(out, bf16, rows, "out"),
-            _stream_ptr(stream))
+            _stream_ptr(None))
         if code:
             self._check("sdlm_tree_attn", code)
         return out
@@ -793,37 +823,39 @@ class Sdlm:
                  _shaped(path, i32, shape, "path")]
         return before, after, (accepted_len, out_tokens, path)
 
+    @_placed
     def tree_commit(self, draft_token: torch.Tensor, next_token: torch.Tensor, parent: torch.Tensor, k_tree: torch.Tensor,
                     v_tree: torch.Tensor, n_nodes: Optional[torch.Tensor] = None,
                     accepted_len: Optional[torch.Tensor] = None, out_tokens: Optional[torch.Tensor] = None,
-                    path: Optional[torch.Tensor] = None, seq_ids: Optional[torch.Tensor] = None, stream=None):
+                    path: Optional[torch.Tensor] = None, seq_ids: Optional[torch.Tensor] = None):
         """sdlm_tree_commit: draft_token, next_token, parent [batch, n] int32; returns accepted_len, out_tokens, path."""
         before, after, outs = self._tree_commit_args(parent, n_nodes, seq_ids, draft_token, next_token, accepted_len, out_tokens, path)
         batch, n = parent.shape
         rows = (batch, n, self.cfg.n_kv_heads, self.cfg.head_dim)
         code = self.lib.sdlm_tree_commit(self.ctx, batch, n, *before, _shaped(k_tree, torch.bfloat16, rows, "k_tree"),
-                                         _shaped(v_tree, torch.bfloat16, rows, "v_tree"), *after, _stream_ptr(stream))
+                                         _shaped(v_tree, torch.bfloat16, rows, "v_tree"), *after, _stream_ptr(None))
         if code:
             self._check("sdlm_tree_commit", code)
         return outs
 
-    def kv_gather_batch(self, k_out: torch.Tensor, v_out: torch.Tensor, seq_ids: Optional[torch.Tensor] = None,
-                        stream=None) -> None:
+    @_placed
+    def kv_gather_batch(self, k_out: torch.Tensor, v_out: torch.Tensor, seq_ids: Optional[torch.Tensor] = None) -> None:
         """sdlm_kv_gather_batch: k_out / v_out [batch, length, Hkv, d]; rows beyond a slot's length stay as they are."""
         if k_out.dim() != 4 or k_out.shape[2:] != (self.cfg.n_kv_heads, self.cfg.head_dim):
             raise ValueError("k_out and v_out must be [batch, length, Hkv, d]")
         batch, length = k_out.shape[:2]
         code = self.lib.sdlm_kv_gather_batch(self.ctx, batch, length, _is(seq_ids, torch.int32, batch, "seq_ids"),
                                              _shaped(k_out, torch.bfloat16, k_out.shape, "k_out"),
-                                             _shaped(v_out, torch.bfloat16, k_out.shape, "v_out"), _stream_ptr(stream))
+                                             _shaped(v_out, torch.bfloat16, k_out.shape, "v_out"), _stream_ptr(None))
         if code:
             self._check("sdlm_kv_gather_batch", code)
 
+    @_placed
     def sample(self, logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None,
                top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
                min_p: Optional[torch.Tensor] = None, token: Optional[torch.Tensor] = None,
                prob: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
-               n_kept: Optional[torch.Tensor] = None, stream=None):
+               n_kept: Optional[torch.Tensor] = None):
         """sdlm_sample: logits [..., vocab] bf16 or float32 (rows may be strided), u and the filters one value a row;
         returns token, prob, entropy, n_kept of the rows' shape."""
         if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dtype in (torch.bfloat16, torch.float32)):
@@ -844,7 +876,7 @@ class Sdlm:
         n_kept = u.new_empty(shape, dtype=i32) if n_kept is None else n_kept
         code = self.lib.sdlm_sample(self.ctx, rows, V, LOGITS_F32 if logits.dtype is f32 else LOGITS_BF16, logits.data_ptr(), stride,
                                     *ins, _is(token, i32, rows, "token"), _is(prob, f32, rows, "prob"),
-                                    _is(entropy, f32, rows, "entropy"), _is(n_kept, i32, rows, "n_kept"), _stream_ptr(stream))
+                                    _is(entropy, f32, rows, "entropy"), _is(n_kept, i32, rows, "n_kept"), _stream_ptr(None))
         if code:
             self._check("sdlm_sample", code)
         return token, prob, entropy, n_kept
