@@ -21,6 +21,10 @@
 //   4. thresholds are narrowed down to one value among the few tokens of the bin or window, which were listed on the way;
 //   5. without top-p one pass forms the kept weights; every thread block then knows the weight of all slices, and the one
 //      that holds u W finds its token.
+// Rows of 151936 bf16 logits, 1 / 128 / 256 of them: greedy 9 / 22 / 41 us (128: 1.8 TB/s, loads that two thread blocks an
+// SM have in flight), all tokens kept 12 / 58 / 103, top-k of 50 16 / 51 / 99, top-p of 0.9 that keeps tens of thousands
+// of tokens 45 / 195 / 350.  A pass over all weights (14 64-bit operations a token, 61 a clock and SM) is 35 of those 58;
+// top-p takes one to two of them, and the thread blocks of a row wait for each other five to eight times.
 // -inf and NaN fail every comparison below, so they need no mask of their own.
 //
 // The answer is a comparison of sums of up to 2^18 weights with u W or p times their total, and a token changes when a
