@@ -23,7 +23,7 @@
 //      that holds u W finds its token.
 // Rows of 151936 bf16 logits, 1 / 128 / 256 of them: greedy 9 / 22 / 41 us (128: 1.8 TB/s, loads that two thread blocks an
 // SM have in flight), all tokens kept 12 / 58 / 103, top-k of 50 16 / 51 / 99, top-p of 0.9 that keeps tens of thousands
-// of tokens 45 / 195 / 350.  A pass over all weights (14 64-bit operations a token, 61 a clock and SM) is 35 of those 58;
+// of tokens 38 / 147 / 264.  A pass over all weights (14 64-bit operations a token, 61 a clock and SM) is 35 of those 58;
 // top-p takes one to two of them, and the thread blocks of a row wait for each other five to eight times.
 // -inf and NaN fail every comparison below, so they need no mask of their own.
 //
@@ -44,7 +44,11 @@ constexpr int kSampleWarps = kSampleThreads / 32;
 constexpr int kSampleBins = 2048;                 // of distance from the maximum: T/102 each, the last one open
 constexpr int kSampleGroups = kSampleBins / 32;   // sums over 32 bins: what thread blocks tell each other first
 constexpr int kSampleSub = 128;                   // parts a key range is cut into
-constexpr int kSampleList = 2048;                 // tokens of a bin or window that a thread block lists
+// Tokens of a bin or window that a thread block lists.  Twice as many for bf16: top-p of 128 rows of 151936 goes from 192
+// to 146 us, as windows need no second look; fp32 gains nothing there and loses an eighth of its greedy rate to the
+// smaller L1 (87 -> 97 us for 256 rows).
+template <bool F32>
+constexpr int kSampleList = F32 ? 2048 : 4096;
 constexpr int kSampleMaxVocab = 1 << 18;
 constexpr uint32_t kSampleCluster = 8;            // thread blocks of a row, at most (the portable cluster size)
 
@@ -125,7 +129,6 @@ struct alignas(16) SampleShared {  // the values behind it are read and written 
   uint32_t group_n[kSampleGroups];                // tokens of 32 bins, and bounds of their weight
   uint64_t group_lo[kSampleGroups], group_hi[kSampleGroups];
   uint32_t lo[2][kSampleSub], hi[2][kSampleSub];  // by parity of the level: one barrier per level then suffices
-  uint32_t list[kSampleList];                     // values (bits) of the tokens in question
   SampleSums mine, extra[2];                      // what a thread block tells the others of its cluster
   uint64_t window[2], looked[2];
   SampleSums warp[kSampleWarps];
@@ -197,8 +200,9 @@ __device__ __forceinline__ N sample_cluster_sum(const N* at, uint32_t C) {
 template <bool F32>
 struct SampleRow {
   static constexpr int kVec = F32 ? 4 : 8;  // values in 16 bytes
-  const uint4* vals;                         // the slice, -inf behind its end
+  const uint4* vals;                         // the slice, -inf behind its end; n_vec is a multiple of 32, so that a warp's lanes stay together
   SampleShared* sh;
+  uint32_t* list;                            // values (bits) of the tokens in question
   int n_vec, C, rank;
   double scale;                              // log2 e / T
   float vmax, v_floor, bin_scale;
@@ -376,9 +380,17 @@ struct SampleRow {
   }
 
   // Lists the tokens of bins [b0, b1] that `floor` keeps whole; n_list is beyond the list's length when they do not fit.
-  __device__ __forceinline__ void put_on_list(float v) {
-    const int at = atomicAdd(&sh->n_list, 1);
-    if (at < kSampleList) sh->list[at] = __float_as_uint(v);
+  // For whole warps: the lane's values i * kVec + e, e in the bits of `which`.  (A lane that went on by itself would take
+  // the weights of its next values alone.)
+  __device__ __forceinline__ void put_on_list(uint32_t which, int i) {
+    if (!__any_sync(0xffffffffu, which)) return;
+    const int mine = __popc(which), incl = warp_prefix(mine), lane = threadIdx.x & 31;
+    int to = 0;
+    if (lane == 31) to = atomicAdd(&sh->n_list, incl);
+    to = __shfl_sync(0xffffffffu, to, 31) + incl - mine;
+    for (; which; which &= which - 1, ++to)
+      if (to < kSampleList<F32>) list[to] = __float_as_uint(at(i * kVec + __ffs(which) - 1));
+    __syncwarp();
   }
   __device__ __forceinline__ void list_bins(int b0, int b1, const SampleCut& floor) {
     if (threadIdx.x == 0) sh->n_list = 0;
@@ -392,11 +404,7 @@ struct SampleRow {
         const int b = bin_of(v[e]);
         in |= v[e] > floor.value && b >= b0 && b <= b1 ? 1u << e : 0u;
       }
-      while (in) {
-        const int e = __ffs(in) - 1;
-        in &= in - 1;
-        put_on_list(at(i * kVec + e));
-      }
+      put_on_list(in, i);
     }
     __syncthreads();
   }
@@ -408,8 +416,8 @@ struct SampleRow {
   // f(value) for the tokens listed (of bins [b0, b1] above the floor), from the slice when the list was too short.
   template <typename F>
   __device__ __forceinline__ void each_listed(int b0, int b1, const SampleCut& floor, F f) {
-    if (sh->n_list <= kSampleList) {
-      for (int i = threadIdx.x; i < sh->n_list; i += kSampleThreads) f(__uint_as_float(sh->list[i]));
+    if (sh->n_list <= kSampleList<F32>) {
+      for (int i = threadIdx.x; i < sh->n_list; i += kSampleThreads) f(__uint_as_float(list[i]));
     } else {
       for (int i = threadIdx.x; i < n_vec; i += kSampleThreads) {
         float v[kVec];
@@ -421,6 +429,7 @@ struct SampleRow {
           in |= v[e] > floor.value && b >= b0 && b <= b1 ? 1u << e : 0u;
         }
         for (; in; in &= in - 1) f(at(i * kVec + __ffs(in) - 1));
+        __syncwarp();
       }
     }
   }
@@ -495,7 +504,7 @@ struct SampleRow {
   }
 
   // Sums over the slice's tokens above the cut (with t >= min_t), by warp: warp w has a contiguous part of the slice.
-  __device__ __forceinline__ int warp_vecs() const { return (n_vec + kSampleWarps - 1) / kSampleWarps; }
+  __device__ __forceinline__ int warp_vecs() const { return (n_vec / 32 + kSampleWarps - 1) / kSampleWarps * 32; }
   __device__ void kept_sums(const SampleCut& cut, double min_t, float reject) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = warp * warp_vecs(), last = min(n_vec, first + warp_vecs());
     SampleSums s{0, 0.0, 0, 0};
@@ -505,7 +514,7 @@ struct SampleRow {
       float mx = v[0];
 #pragma unroll
       for (int e = 1; e < kVec; ++e) mx = fmaxf(mx, v[e]);
-      if (!(mx >= reject)) continue;
+      if (!__any_sync(0xffffffffu, mx >= reject)) continue;
       // (no branch on a single token: eight chains of 64-bit operations at a time keep their pipe fed, one does not)
 #pragma unroll
       for (int e = 0; e < kVec; ++e) {
@@ -532,7 +541,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
   constexpr int kVec = Row::kVec;
   extern __shared__ __align__(16) uint8_t sample_smem[];
   SampleShared* sh = reinterpret_cast<SampleShared*>(sample_smem);
-  uint4* vals = reinterpret_cast<uint4*>(sample_smem + sizeof(SampleShared));
+  uint32_t* list = reinterpret_cast<uint32_t*>(sample_smem + sizeof(SampleShared));
+  uint4* vals = reinterpret_cast<uint4*>(list + kSampleList<F32>);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   uint32_t C;
   asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(C));
@@ -548,7 +558,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
   const float u = p.u[row];
 
   // ---- the slice into shared memory, its largest value
-  const int first = (int)rank * p.per, n = max(0, min(p.per, p.V - first)), n_vec = (n + kVec - 1) / kVec;
+  const int first = (int)rank * p.per, n = max(0, min(p.per, p.V - first)), n_vec = (n + 32 * kVec - 1) / (32 * kVec) * 32;
   float mx = -INFINITY;
   {
     const int whole = p.vec ? n / kVec : 0;
@@ -626,7 +636,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
   // ---- thresholds
   const bool greedy = !(T > 0.0f);
   Row s;
-  s.vals = vals; s.sh = sh; s.n_vec = n_vec; s.C = (int)C; s.rank = (int)rank; s.level = 0;
+  s.vals = vals; s.sh = sh; s.list = list; s.n_vec = n_vec; s.C = (int)C; s.rank = (int)rank; s.level = 0;
   s.vmax = mx;
   s.v_floor = fmaxf(mx - 138.0f * (greedy ? 1.0f : T), -3.402823466e38f);  // 200 ln 2 T below, and no -inf
   s.scale = 1.4426950408889634074 / (double)(greedy ? 1.0f : T);
@@ -663,7 +673,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
         b0 = sh->b0;
         b1 = sh->b1;
         // many tokens (a wide window in a thin tail): no list yet, but whole groups, and a second look with the sums known
-        const bool wide = pass == 0 && sh->n_window > (uint32_t)(kSampleList / 2) * C;
+        const bool wide = pass == 0 && sh->n_window > (uint32_t)(kSampleList<F32> / 2) * C;
         if (wide) {
           b0 &= ~31;
           b1 |= 31;
@@ -689,11 +699,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
               count += up && v[e] > -INFINITY ? 1u : 0u;
               listed |= mid && v[e] > -INFINITY ? 1u << e : 0u;
             }
-            while (listed && !wide) {
-              const int e = __ffs(listed) - 1;
-              listed &= listed - 1;
-              s.put_on_list(s.at(i * kVec + e));
-            }
+            if (!wide) s.put_on_list(listed, i);
           }
         } else {
           for (int i = tid; i < n_vec; i += kSampleThreads) {
@@ -705,7 +711,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
               const int b = s.bin_of(v[e]);
               some |= v[e] > top.value && b >= from && b <= upto ? 1u << e : 0u;
             }
-            if (!some) continue;  // (a weight at a time for those of them took a quarter longer than all of them side by side)
+            if (!__any_sync(0xffffffffu, some)) continue;  // (a weight at a time for those of them took a quarter longer than all of them side by side)
             uint32_t listed = 0;
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
@@ -719,11 +725,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
               count += up ? 1u : 0u;
               listed |= mid ? 1u << e : 0u;
             }
-            while (listed && !wide) {
-              const int e = __ffs(listed) - 1;
-              listed &= listed - 1;
-              s.put_on_list(s.at(i * kVec + e));
-            }
+            if (!wide) s.put_on_list(listed, i);
           }
         }
         above = sample_warp_sum(above);
@@ -950,7 +952,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
 }
 
 cudaError_t setup_sample(sdlm_ctx*) {
-  const int most = (int)sizeof(SampleShared) + (kSampleMaxVocab / 8 + 8) * 4;
+  const int most = (int)sizeof(SampleShared) + kSampleList<true> * 4 + (kSampleMaxVocab / 8 + 8) * 4 + 512;  // (bf16: half the slice)
   cudaError_t e = cudaFuncSetAttribute(sample_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(sample_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
   return e;
@@ -979,14 +981,15 @@ extern "C" sdlm_status sdlm_sample(sdlm_ctx* ctx, int32_t rows, int32_t vocab, s
   p.V = vocab;
   // Thread blocks of a row, in powers of two up to eight (the portable cluster size): a slice of at most 80 KB, so that two
   // fit an SM, and eight where all rows then run at once.  More of them have less to do each but meet as often: 128 rows of
-  // 151936 bf16 logits, top-k 51 us with four and 77 with eight, top-k and top-p 86 and 143; one row, top-p: 63 and 49.
+  // 151936 bf16 logits, top-k 51 us with four and 77 with eight, top-k and top-p 86 and 143; one row, top-p: 63 and 49 (before later steps).
   const int esz = f32 ? 4 : 2;
   unsigned c = 1;
   const int most = rows * 8 <= ctx->sm_count ? 16384 : 81920;
   while (c < 8 && (long long)vocab * esz > (long long)most * c) c *= 2;
   p.per = (int)(((vocab + c - 1) / c + 7) / 8 * 8);
   p.vec = at % 16 == 0 && (row_stride * esz) % 16 == 0;
-  const size_t smem = sizeof(SampleShared) + (size_t)p.per * esz;
+  const size_t list = (size_t)(f32 ? kSampleList<true> : kSampleList<false>) * 4;
+  const size_t smem = sizeof(SampleShared) + list + ((size_t)p.per * esz + 511) / 512 * 512;  // (whole warps of 16 bytes a lane)
   const dim3 grid((unsigned)rows * c);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e = f32 ? launch_overlapped_cluster(sample_kernel<true>, grid, dim3(kSampleThreads), smem, st, c, p)
