@@ -73,14 +73,12 @@ def tree_commit_layers(contexts, draft_token, next_token, parent, k_trees, v_tre
     n_layers = len(contexts)
     if len(k_trees) != n_layers or len(v_trees) != n_layers:
         raise ValueError("k_trees and v_trees must hold one tensor per context")
-    for t in (draft_token, next_token, parent, n_nodes, accepted_len, out_tokens, path, seq_ids, *k_trees, *v_trees):
-        if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != sd0.device_index:
-            raise ValueError(f"a tensor is on GPU {t.get_device()}, the contexts on GPU {sd0.device_index}")
+    gpu = sd0.device_index
     before, after, outs = sd0._tree_commit_args(parent, n_nodes, seq_ids, draft_token, next_token, accepted_len, out_tokens, path)
     rows = (*parent.shape, sd0.cfg.n_kv_heads, sd0.cfg.head_dim)
     ctx_arr = (C.c_void_p * n_layers)(*[c.ctx.value for c in contexts])
-    k_arr = (C.c_void_p * n_layers)(*[_shaped(t, torch.bfloat16, rows, "k_tree") for t in k_trees])
-    v_arr = (C.c_void_p * n_layers)(*[_shaped(t, torch.bfloat16, rows, "v_tree") for t in v_trees])
+    k_arr = (C.c_void_p * n_layers)(*[_shaped(t, torch.bfloat16, rows, "k_tree", gpu) for t in k_trees])
+    v_arr = (C.c_void_p * n_layers)(*[_shaped(t, torch.bfloat16, rows, "v_tree", gpu) for t in v_trees])
     sd0._check("sdlm_tree_commit_layers", sd0.lib.sdlm_tree_commit_layers(
         ctx_arr, n_layers, *parent.shape, *before, k_arr, v_arr, *after, _stream_ptr(None)))
     return outs
@@ -286,10 +284,12 @@ def _host(t: torch.Tensor, dtype, name: str) -> torch.Tensor:
     return t
 
 
-def _row_stride(t: torch.Tensor, d: int, name: str) -> int:
+def _row_stride(t: torch.Tensor, d: int, name: str, gpu: int) -> int:
     """Elements between the rows of a [batch, D, heads, d] tensor whose rows are evenly spaced, heads contiguous."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.bfloat16 and t.dim() == 4 and t.shape[3] == d):
         raise TypeError(f"{name}: expected a CUDA tensor of torch.bfloat16, [batch, D, heads, {d}]")
+    if t.get_device() != gpu:
+        _refuse(t, torch.bfloat16, name, gpu)
     batch, D, heads, _ = t.shape
     st = t.stride()
     if st[3] != 1 or (heads > 1 and st[2] != d):
@@ -313,38 +313,37 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
 
 def _placed(call):
     """For calls that make their outputs: with `stream` the call runs with that stream current, so that the outputs are
-    allocated (and cleared) on it too; tensors of another GPU than the context's are refused."""
+    allocated (and cleared) on it too."""
     @functools.wraps(call)
     def placed(self, *args, stream=None, **kw):
-        if stream is not None:
-            with torch.cuda.stream(stream):
-                return placed(self, *args, **kw)
-        index = self.device_index
-        for t in args:
-            if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != index:
-                raise ValueError(f"a tensor is on GPU {t.get_device()}, the context on GPU {index}")
-        for name, t in kw.items():
-            if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != index:
-                raise ValueError(f"{name} is on GPU {t.get_device()}, the context on GPU {index}")
-        return call(self, *args, **kw)
+        if stream is None:
+            return call(self, *args, **kw)
+        with torch.cuda.stream(stream):
+            return call(self, *args, **kw)
     return placed
 
 
-def _is(t, dtype, numel: int, name: str) -> int:
-    """Address of a contiguous CUDA tensor of `numel` elements of dtype; None stays None."""
+def _refuse(t, dtype, name: str, gpu: int):
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != gpu:
+        raise ValueError(f"{name} is on GPU {t.get_device()}, the context on GPU {gpu}")
+    raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}")
+
+
+def _is(t, dtype, numel: int, name: str, gpu: int) -> int:
+    """Address of a contiguous tensor of `numel` elements of dtype on that GPU; None stays None."""
     if t is None:
         return None
-    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.is_contiguous()):
-        raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}")
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == gpu and t.is_contiguous()):
+        _refuse(t, dtype, name, gpu)
     if t.numel() != numel:
         raise ValueError(f"{name}: expected {numel} elements")
     return t.data_ptr()
 
 
-def _shaped(t, dtype, shape, name: str) -> int:
-    """Address of a contiguous CUDA tensor of that shape."""
-    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.is_contiguous()):
-        raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}")
+def _shaped(t, dtype, shape, name: str, gpu: int) -> int:
+    """Address of a contiguous tensor of that shape on that GPU."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == gpu and t.is_contiguous()):
+        _refuse(t, dtype, name, gpu)
     if t.shape != shape:
         raise ValueError(f"{name}: expected the shape {tuple(shape)}")
     return t.data_ptr()
@@ -757,26 +756,26 @@ class Sdlm:
                      seq_ids: Optional[torch.Tensor] = None):
         """sdlm_qk_norm_rope: q [batch, D, n_heads, d] and k [batch, D, n_heads2, d] or None; either may be a slice of
         the heads of a wider tensor (a stacked q/k/v product)."""
-        d = self.cfg.head_dim
-        q_stride = _row_stride(q, d, "q")
+        d, gpu = self.cfg.head_dim, self.device_index
+        q_stride = _row_stride(q, d, "q", gpu)
         batch, D, heads, _ = q.shape
         heads2 = k_stride = 0
         k_ptr = k_out_ptr = None
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
         if k is not None:
-            k_stride = _row_stride(k, d, "k")
+            k_stride = _row_stride(k, d, "k", gpu)
             if k.shape[0] != batch or k.shape[1] != D:
                 raise ValueError("q and k must have the same rows")
             heads2, k_ptr = k.shape[2], k.data_ptr()
             if k_out is None:
                 k_out = torch.empty(k.shape, dtype=torch.bfloat16, device=self.device)
-            k_out_ptr = _shaped(k_out, torch.bfloat16, k.shape, "k_out")
+            k_out_ptr = _shaped(k_out, torch.bfloat16, k.shape, "k_out", gpu)
         code = self.lib.sdlm_qk_norm_rope(
-            self.ctx, batch, D, _is(seq_ids, torch.int32, batch, "seq_ids"), _is(positions, torch.int32, batch * D, "positions"),
+            self.ctx, batch, D, _is(seq_ids, torch.int32, batch, "seq_ids", gpu), _is(positions, torch.int32, batch * D, "positions", gpu),
             1 if relative else 0, C.byref(rope.to_c()), eps, heads, q.data_ptr(), q_stride,
-            _is(q_weight, torch.bfloat16, d, "q_weight"), _shaped(q_out, torch.bfloat16, q.shape, "q_out"), heads2, k_ptr, k_stride,
-            _is(k_weight, torch.bfloat16, d, "k_weight"), k_out_ptr, _stream_ptr(None))
+            _is(q_weight, torch.bfloat16, d, "q_weight", gpu), _shaped(q_out, torch.bfloat16, q.shape, "q_out", gpu), heads2, k_ptr, k_stride,
+            _is(k_weight, torch.bfloat16, d, "k_weight", gpu), k_out_ptr, _stream_ptr(None))
         if code:
             self._check("sdlm_qk_norm_rope", code)
         return q_out, k_out
@@ -796,12 +795,12 @@ class Sdlm:
         if out is None:
             out = torch.empty_like(q) if n_nodes is None and seq_ids is None else torch.zeros_like(q)
         batch, n = self._tree_shape(parent)
-        c, bf16 = self.cfg, torch.bfloat16
+        c, bf16, gpu = self.cfg, torch.bfloat16, self.device_index
         rows, kv_rows = (batch, n, c.n_q_heads, c.head_dim), (batch, n, c.n_kv_heads, c.head_dim)
         code = self.lib.sdlm_tree_attn(
-            self.ctx, batch, n, _is(seq_ids, torch.int32, batch, "seq_ids"), _is(n_nodes, torch.int32, batch, "n_nodes"),
-            _shaped(parent, torch.int32, (batch, n), "parent"), _shaped(q, bf16, rows, "q"),
-            _shaped(k_tree, bf16, kv_rows, "k_tree"), _shaped(v_tree, bf16, kv_rows, "v_tree"), _shaped(out, bf16, rows, "out"),
+            self.ctx, batch, n, _is(seq_ids, torch.int32, batch, "seq_ids", gpu), _is(n_nodes, torch.int32, batch, "n_nodes", gpu),
+            _shaped(parent, torch.int32, (batch, n), "parent", gpu), _shaped(q, bf16, rows, "q", gpu),
+            _shaped(k_tree, bf16, kv_rows, "k_tree", gpu), _shaped(v_tree, bf16, kv_rows, "v_tree", gpu), _shaped(out, bf16, rows, "out", gpu),
             _stream_ptr(None))
         if code:
             self._check("sdlm_tree_attn", code)
@@ -810,17 +809,17 @@ class Sdlm:
     def _tree_commit_args(self, parent, n_nodes, seq_ids, draft_token, next_token, accepted_len, out_tokens, path):
         """Checked outputs (made here where they are None) and the addresses in the order of the C call's arguments."""
         batch, n = shape = self._tree_shape(parent)
-        i32 = torch.int32
+        i32, gpu = torch.int32, self.device_index
         if accepted_len is None:
             accepted_len = parent.new_empty(batch)
         if out_tokens is None:
             out_tokens = torch.empty_like(parent)
         if path is None:
             path = torch.empty_like(parent)
-        before = [_is(seq_ids, i32, batch, "seq_ids"), _is(n_nodes, i32, batch, "n_nodes"), _shaped(parent, i32, shape, "parent"),
-                  _shaped(draft_token, i32, shape, "draft_token"), _shaped(next_token, i32, shape, "next_token")]
-        after = [_is(accepted_len, i32, batch, "accepted_len"), _shaped(out_tokens, i32, shape, "out_tokens"),
-                 _shaped(path, i32, shape, "path")]
+        before = [_is(seq_ids, i32, batch, "seq_ids", gpu), _is(n_nodes, i32, batch, "n_nodes", gpu), _shaped(parent, i32, shape, "parent", gpu),
+                  _shaped(draft_token, i32, shape, "draft_token", gpu), _shaped(next_token, i32, shape, "next_token", gpu)]
+        after = [_is(accepted_len, i32, batch, "accepted_len", gpu), _shaped(out_tokens, i32, shape, "out_tokens", gpu),
+                 _shaped(path, i32, shape, "path", gpu)]
         return before, after, (accepted_len, out_tokens, path)
 
     @_placed
@@ -830,10 +829,11 @@ class Sdlm:
                     path: Optional[torch.Tensor] = None, seq_ids: Optional[torch.Tensor] = None):
         """sdlm_tree_commit: draft_token, next_token, parent [batch, n] int32; returns accepted_len, out_tokens, path."""
         before, after, outs = self._tree_commit_args(parent, n_nodes, seq_ids, draft_token, next_token, accepted_len, out_tokens, path)
+        gpu = self.device_index
         batch, n = parent.shape
         rows = (batch, n, self.cfg.n_kv_heads, self.cfg.head_dim)
-        code = self.lib.sdlm_tree_commit(self.ctx, batch, n, *before, _shaped(k_tree, torch.bfloat16, rows, "k_tree"),
-                                         _shaped(v_tree, torch.bfloat16, rows, "v_tree"), *after, _stream_ptr(None))
+        code = self.lib.sdlm_tree_commit(self.ctx, batch, n, *before, _shaped(k_tree, torch.bfloat16, rows, "k_tree", gpu),
+                                         _shaped(v_tree, torch.bfloat16, rows, "v_tree", gpu), *after, _stream_ptr(None))
         if code:
             self._check("sdlm_tree_commit", code)
         return outs
@@ -843,10 +843,11 @@ class Sdlm:
         """sdlm_kv_gather_batch: k_out / v_out [batch, length, Hkv, d]; rows beyond a slot's length stay as they are."""
         if k_out.dim() != 4 or k_out.shape[2:] != (self.cfg.n_kv_heads, self.cfg.head_dim):
             raise ValueError("k_out and v_out must be [batch, length, Hkv, d]")
+        gpu = self.device_index
         batch, length = k_out.shape[:2]
-        code = self.lib.sdlm_kv_gather_batch(self.ctx, batch, length, _is(seq_ids, torch.int32, batch, "seq_ids"),
-                                             _shaped(k_out, torch.bfloat16, k_out.shape, "k_out"),
-                                             _shaped(v_out, torch.bfloat16, k_out.shape, "v_out"), _stream_ptr(None))
+        code = self.lib.sdlm_kv_gather_batch(self.ctx, batch, length, _is(seq_ids, torch.int32, batch, "seq_ids", gpu),
+                                             _shaped(k_out, torch.bfloat16, k_out.shape, "k_out", gpu),
+                                             _shaped(v_out, torch.bfloat16, k_out.shape, "v_out", gpu), _stream_ptr(None))
         if code:
             self._check("sdlm_kv_gather_batch", code)
 
@@ -867,16 +868,18 @@ class Sdlm:
                 raise TypeError("logits: only the rows of [rows, vocab] may be strided")
             if rows > 1:
                 stride = logits.stride(0)
-        f32, i32 = torch.float32, torch.int32
-        ins = [_is(u, f32, rows, "u"), _is(temperature, f32, rows, "temperature"), _is(top_k, i32, rows, "top_k"),
-               _is(top_p, f32, rows, "top_p"), _is(min_p, f32, rows, "min_p")]
+        f32, i32, gpu = torch.float32, torch.int32, self.device_index
+        if logits.get_device() != gpu:
+            _refuse(logits, logits.dtype, "logits", gpu)
+        ins = [_is(u, f32, rows, "u", gpu), _is(temperature, f32, rows, "temperature", gpu), _is(top_k, i32, rows, "top_k", gpu),
+               _is(top_p, f32, rows, "top_p", gpu), _is(min_p, f32, rows, "min_p", gpu)]
         token = u.new_empty(shape, dtype=i32) if token is None else token
         prob = u.new_empty(shape) if prob is None else prob
         entropy = u.new_empty(shape) if entropy is None else entropy
         n_kept = u.new_empty(shape, dtype=i32) if n_kept is None else n_kept
         code = self.lib.sdlm_sample(self.ctx, rows, V, LOGITS_F32 if logits.dtype is f32 else LOGITS_BF16, logits.data_ptr(), stride,
-                                    *ins, _is(token, i32, rows, "token"), _is(prob, f32, rows, "prob"),
-                                    _is(entropy, f32, rows, "entropy"), _is(n_kept, i32, rows, "n_kept"), _stream_ptr(None))
+                                    *ins, _is(token, i32, rows, "token", gpu), _is(prob, f32, rows, "prob", gpu),
+                                    _is(entropy, f32, rows, "entropy", gpu), _is(n_kept, i32, rows, "n_kept", gpu), _stream_ptr(None))
         if code:
             self._check("sdlm_sample", code)
         return token, prob, entropy, n_kept

@@ -711,7 +711,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
               const int b = s.bin_of(v[e]);
               some |= v[e] > top.value && b >= from && b <= upto ? 1u << e : 0u;
             }
-            if (!__any_sync(0xffffffffu, some)) continue;  // (a weight at a time for those of them took a quarter longer than all of them side by side)
+            if (!__any_sync(0xffffffffu, some)) continue;  // (a weight at a time instead: bf16 6 % faster, fp32 2 % slower)
             uint32_t listed = 0;
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
