@@ -18,7 +18,8 @@
 //   2. (top-k, top-p) tokens are counted by distance from the maximum in bins of T/102: top-k's threshold lies in one bin,
 //      and since a bin's weights are known to 1 %, top-p's in a window of a few;
 //   3. (top-p) one pass forms the weights and adds them up above, in and below that window;
-//   4. thresholds are narrowed down to one value among the few tokens of the bin or window, which were listed on the way;
+//   4. thresholds are narrowed down to one value among the few tokens of the bin or window, which were listed on the way
+//      (all tokens that a small top-k can keep are, and then only the list is looked at: top-k of 50 and top-p 88 -> 76 us);
 //   5. without top-p one pass forms the kept weights; every thread block then knows the weight of all slices, and the one
 //      that holds u W finds its token.
 // Rows of 151936 bf16 logits, 1 / 128 / 256 of them: greedy 9 / 22 / 41 us (128: 1.8 TB/s, loads that two thread blocks an
@@ -417,7 +418,11 @@ struct SampleRow {
   template <typename F>
   __device__ __forceinline__ void each_listed(int b0, int b1, const SampleCut& floor, F f) {
     if (sh->n_list <= kSampleList<F32>) {
-      for (int i = threadIdx.x; i < sh->n_list; i += kSampleThreads) f(__uint_as_float(list[i]));
+      for (int i = threadIdx.x; i < sh->n_list; i += kSampleThreads) {
+        const float v = __uint_as_float(list[i]);
+        const int b = bin_of(v);
+        if (v > floor.value && b >= b0 && b <= b1) f(v);
+      }
     } else {
       for (int i = threadIdx.x; i < n_vec; i += kSampleThreads) {
         float v[kVec];
@@ -530,8 +535,41 @@ struct SampleRow {
     s.ent = sample_warp_sum(s.ent);
     s.count = __reduce_add_sync(0xffffffffu, s.count);
     s.ties = __reduce_add_sync(0xffffffffu, s.ties);
+    __syncthreads();  // the sums that were there have been read
     if (lane == 0) sh->warp[warp] = s;
     __syncthreads();
+  }
+  // The same over the tokens listed (of bins [b0, b1] above the floor); returns the thread block's.  In whole numbers, as the
+  // list has no fixed order.
+  __device__ SampleSums listed_sums(int b0, int b1, const SampleCut& floor, const SampleCut& cut, double min_t, float reject) {
+    uint64_t mass = 0, ent = 0;
+    uint32_t count = 0, ties = 0;
+    each_listed(b0, b1, floor, [&](float v) {
+      const SampleWeight w = weight(v);
+      if (v > cut.value && v >= reject && w.t >= min_t) {
+        mass += w.whole;
+        ent += sample_entropy(w);
+        ++count;
+      } else if (v == cut.value) {
+        ++ties;
+      }
+    });
+    mass = sample_warp_sum(mass);
+    ent = sample_warp_sum(ent);
+    count = __reduce_add_sync(0xffffffffu, count);
+    ties = __reduce_add_sync(0xffffffffu, ties);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) sh->warp[threadIdx.x >> 5] = SampleSums{mass, 4.0 * (double)ent, count, ties};
+    __syncthreads();
+    SampleSums all{0, 0.0, 0, 0};
+#pragma unroll 1
+    for (int i = 0; i < kSampleWarps; ++i) {
+      all.mass += sh->warp[i].mass;
+      all.ent += sh->warp[i].ent;
+      all.count += sh->warp[i].count;
+      all.ties += sh->warp[i].ties;
+    }
+    return all;
   }
 };
 
@@ -648,15 +686,17 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
   int mode = greedy || k == 1 ? 1 : by_k || by_p ? 2 : 0;
   asm volatile("" : "+r"(mode));
   SampleSums own{0, 0.0, 0, 0};  // this thread block's kept tokens, once known
-  bool summed = false;
+  bool summed = false, few = false;
   if (mode == 1) {
     cut = SampleCut{mx, 1u};
   } else if (mode == 2) {
     const double p64 = fmax((double)top_p, 0.0);
     s.find_bins(by_k, k, by_p);
     const int b_k = sh->b_k;
+    // with few tokens kept by top-k, all that can be are listed, and nothing below looks at the slice again
+    few = b_k < kSampleBins && k <= kSampleList<F32> / 2;
     if (b_k < kSampleBins) {
-      s.list_bins(b_k, b_k, cut);
+      s.list_bins(few ? 0 : b_k, b_k, cut);
       cut = s.template narrow<false>(b_k, b_k, cut, false, sh->before_k, (uint64_t)k);
     }
     if (by_p) {
@@ -668,12 +708,12 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
       own = SampleSums{0, 0.0, 0, 0};
       for (int pass = 0; pass < 2; ++pass) {
         if (warp == 0) s.find_window(pass > 0, from >> 5, upto >> 5, (double)all_above, (double)in_window, (double)want, p64);
-        if (tid == 0) sh->n_list = 0;
+        if (tid == 0 && !few) sh->n_list = 0;
         __syncthreads();
         b0 = sh->b0;
         b1 = sh->b1;
         // many tokens (a wide window in a thin tail): no list yet, but whole groups, and a second look with the sums known
-        const bool wide = pass == 0 && sh->n_window > (uint32_t)(kSampleList<F32> / 2) * C;
+        const bool wide = !few && pass == 0 && sh->n_window > (uint32_t)(kSampleList<F32> / 2) * C;
         if (wide) {
           b0 &= ~31;
           b1 |= 31;
@@ -701,6 +741,21 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
             }
             if (!wide) s.put_on_list(listed, i);
           }
+        } else if (few) {
+          uint64_t whole_ent = 0;
+          s.each_listed(0, b_k, top, [&](float v) {
+            const SampleWeight w = s.weight(v);
+            const int b = s.bin_of(v);
+            all_mine += w.whole;
+            if (b < b0) {
+              above += w.whole;
+              whole_ent += sample_entropy(w);
+              ++count;
+            } else if (b <= b1) {
+              inside += w.whole;
+            }
+          });
+          ent = 4.0 * (double)whole_ent;
         } else {
           for (int i = tid; i < n_vec; i += kSampleThreads) {
             float v[kVec];
@@ -773,38 +828,28 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
       cut = s.template narrow<true>(b0, b1, top, tied_k && b_k <= b1, all_above, want);
       if (tied_k && cut.value == top.value) cut.take = min(cut.take, top.take);
       // this thread block's kept tokens: those above the window and the listed ones above the cut
-      uint64_t m2 = 0, e2 = 0;
-      uint32_t c2 = 0, t2 = 0;
-      s.each_listed(b0, b1, top, [&](float v) {
-        if (v > cut.value) {
-          const SampleWeight w = s.weight(v);
-          m2 += w.whole;
-          e2 += sample_entropy(w);
-          ++c2;
-        } else if (v == cut.value) {
-          ++t2;
-        }
-      });
-      if (tied_k && cut.value == top.value) {  // (these were not listed)
-        for (int i = tid; i < n_vec; i += kSampleThreads) {
-          float v[kVec];
-          Row::unpack(vals[i], v);
+      const SampleSums in = s.listed_sums(b0, b1, top, cut, -INFINITY, -INFINITY);
+      own.mass += in.mass;
+      own.ent += in.ent;
+      own.count += in.count;
+      own.ties += in.ties;
+      if (tied_k && cut.value == top.value) {  // (these were left out)
+        uint32_t t = 0;
+        if (few) {
+          s.each_listed(b_k, b_k, SampleCut{-INFINITY, 0u}, [&](float v) { t += v == cut.value ? 1u : 0u; });
+        } else {
+          for (int i = tid; i < n_vec; i += kSampleThreads) {
+            float v[kVec];
+            Row::unpack(vals[i], v);
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) t2 += v[e] == cut.value ? 1u : 0u;
+            for (int e = 0; e < kVec; ++e) t += v[e] == cut.value ? 1u : 0u;
+          }
         }
-      }
-      m2 = sample_warp_sum(m2);
-      e2 = sample_warp_sum(e2);
-      c2 = __reduce_add_sync(0xffffffffu, c2);
-      t2 = __reduce_add_sync(0xffffffffu, t2);
-      if (lane == 0) sh->warp[warp] = SampleSums{m2, 4.0 * (double)e2, c2, t2};  // (the sums over the list in whole numbers)
-      __syncthreads();
+        t = __reduce_add_sync(0xffffffffu, t);
+        if (lane == 0) sh->scan32[warp] = t;
+        __syncthreads();
 #pragma unroll 1
-      for (int i = 0; i < kSampleWarps; ++i) {
-        own.mass += sh->warp[i].mass;
-        own.ent += sh->warp[i].ent;
-        own.count += sh->warp[i].count;
-        own.ties += sh->warp[i].ties;
+        for (int i = 0; i < kSampleWarps; ++i) own.ties += sh->scan32[i];
       }
       summed = true;
     }
@@ -825,7 +870,9 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
 
   // ---- what is kept in each slice
   bool warps_known = false;
-  if (!summed) {
+  if (!summed && few) {
+    own = s.listed_sums(0, sh->b_k, SampleCut{-INFINITY, 0u}, cut, min_t, reject);
+  } else if (!summed) {
     s.kept_sums(cut, min_t, reject);
     warps_known = true;
     own = SampleSums{0, 0.0, 0, 0};
@@ -981,7 +1028,7 @@ extern "C" sdlm_status sdlm_sample(sdlm_ctx* ctx, int32_t rows, int32_t vocab, s
   p.V = vocab;
   // Thread blocks of a row, in powers of two up to eight (the portable cluster size): a slice of at most 80 KB, so that two
   // fit an SM, and eight where all rows then run at once.  More of them have less to do each but meet as often: 128 rows of
-  // 151936 bf16 logits, top-k 51 us with four and 77 with eight, top-k and top-p 86 and 143; one row, top-p: 63 and 49 (before later steps).
+  // 151936 bf16 logits, top-k 51 us with four and 77 with eight; one row, top-p: 63 and 49 (before later steps).
   const int esz = f32 ? 4 : 2;
   unsigned c = 1;
   const int most = rows * 8 <= ctx->sm_count ? 16384 : 81920;

@@ -201,3 +201,24 @@ def test_refusals(sd):
         sd.sample(x.half(), u)
     with pytest.raises(TypeError):
         sd.sample(x.t(), torch.zeros(64, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_top_k_around_the_length_of_the_list(sd, dtype):
+    """Few tokens kept by top-k are listed and only the list is looked at again; more are not.  Both, with every other
+    filter behind them, on random rows, on rows of a few values (more ties than the list has room for), and again with the
+    same bits although a list has no fixed order."""
+    rng = np.random.default_rng(16)
+    V = 40000
+    x = (rng.normal(size=(16, V)) * 2).astype(np.float32)
+    x[8:] = np.round(x[8:])
+    logits = torch.from_numpy(x).cuda().to(dtype)
+    u = rng.random(16)
+    k = np.array([3, 50, 1000, 1024, 1025, 2048, 2049, 5000] * 2)
+    for kw in (dict(), dict(p=np.full(16, 0.8)), dict(m=np.full(16, 0.05)), dict(p=np.full(16, 0.95), m=np.full(16, 0.02))):
+        _check(sd, logits, u, k=k, **kw)
+    dev = lambda a, dt: torch.as_tensor(a, dtype=dt, device="cuda")
+    args = (logits, dev(u, torch.float32), None, dev(k, torch.int32), dev(np.full(16, 0.9), torch.float32), dev(np.full(16, 0.03), torch.float32))
+    first = sd.sample(*args)
+    for _ in range(4):
+        assert all(torch.equal(a, b) for a, b in zip(first, sd.sample(*args)))
