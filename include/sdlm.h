@@ -513,7 +513,7 @@ sdlm_status sdlm_qk_norm_rope(sdlm_ctx* ctx, int32_t batch, int32_t D, const int
  *   nodes on the path of node j and j itself.
  * q, out [batch, n, Hq, d]; k_tree / v_tree [batch, n, Hkv, d]: device bf16; parent device int32 [batch, n].
  * 1 <= n <= 64; any Hq/Hkv; max_block does not limit n.  n = 1 is attention of a single token.  Slots may repeat.
- * K and V of the tree's nodes have to be finite.  fp32 scores, sums and accumulation, weights rounded to bf16 before
+ * K and V of the tree's nodes have to be finite; out must not overlap q, k_tree or v_tree.  fp32 scores, sums and accumulation, weights rounded to bf16 before
  * they meet V, bf16 output; results do not depend on timing.  The cache is not modified.
  * Uses workspace scratch: calls on one context must not overlap on the GPU.
  * Errors: INVALID_ARG, SHAPE (batch, n, or a schedule beyond 32 bits), UNSUPPORTED (softmax_scale not positive), CUDA. */
@@ -528,7 +528,8 @@ sdlm_status sdlm_tree_attn(sdlm_ctx* ctx, int32_t batch, int32_t n, const int32_
  * nodes in order, -1 behind them; accepted_len[b] = their number (at least 1; 0 without nodes); out_tokens [batch, n]:
  * next_token of the path's nodes, -1 behind them; rows path[b, 0..accepted_len[b]) of k_tree / v_tree
  * [batch, n, Hkv, d] are appended to the cache as sdlm_accept_commit appends its rows.  A sequence that fails
- * commits nothing: accepted_len[b] = -1, its out_tokens are -1.
+ * commits nothing: accepted_len[b] = -1, its out_tokens are -1.  The outputs must overlap neither each other nor
+ * draft_token, next_token and parent.
  * The _layers form commits into several caches (as sdlm_accept_commit_layers; distinct contexts).
  * Uses workspace scratch of the (first) context.
  * Errors: as sdlm_accept_commit(_layers); n <= 64.  Device status: OUT_OF_PAGES, DEVICE_CHECK (also for a slot that

@@ -1315,6 +1315,13 @@ static sdlm_status tree_commit_launch(sdlm_ctx* const* ctxs, int32_t n_layers, i
   sdlm_ctx* c0 = ctxs[0];
   if (!c0) return SDLM_ERR_INVALID_ARG;
   if (batch > c0->cfg.max_batch) return SDLM_ERR_SHAPE;
+  // the outputs are written while tokens and parents of the same tree are still read, in another order
+  const size_t nodes_b = (size_t)batch * n * 4;
+  for (const int32_t* in : {parent, draft_token, next_token})
+    if (ranges_overlap(out_tokens, nodes_b, in, nodes_b) || ranges_overlap(path, nodes_b, in, nodes_b) ||
+        ranges_overlap(accepted_len, (size_t)batch * 4, in, nodes_b))
+      return SDLM_ERR_INVALID_ARG;
+  if (ranges_overlap(path, nodes_b, out_tokens, nodes_b)) return SDLM_ERR_INVALID_ARG;
   CommitLayers* L = new (std::nothrow) CommitLayers;
   if (!L) return SDLM_ERR_CUDA;
   for (int l = 0; l < n_layers; ++l) {

@@ -171,6 +171,12 @@ inline cudaError_t launch_overlapped_cluster(void (*kernel)(KArgs...), dim3 grid
   return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
 }
 
+// Whether [a, a + an) and [b, b + bn) (bytes) share any.
+inline bool ranges_overlap(const void* a, size_t an, const void* b, size_t bn) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + bn && y < x + an;
+}
+
 // Whether the context's device is the current one: its memory and its streams are that device's.
 inline bool same_device(const sdlm_ctx* ctx) {
   int dev = -1;

@@ -200,12 +200,6 @@ static bool rope_frequencies(const sdlm_rope& r, int rot, double* freq, float* m
 
 static inline bool rope_a16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// Whether [a, a + an) and [b, b + bn) (bytes) share any.
-static inline bool rope_overlap(const void* a, size_t an, const void* b, size_t bn) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + bn && y < x + an;
-}
-
 }  // namespace sdlm
 
 using namespace sdlm;
@@ -247,9 +241,9 @@ extern "C" sdlm_status sdlm_qk_norm_rope(sdlm_ctx* ctx, int32_t batch, int32_t D
   // Rows may be rotated in place (out is x, dense rows); any other overlap would have rows read after they are written.
   const size_t qn = ((size_t)(rows - 1) * q_stride + qw) * 2, kn = k ? ((size_t)(rows - 1) * k_stride + kw) * 2 : 0;
   const size_t qo = (size_t)rows * qw * 2, ko = (size_t)rows * kw * 2;
-  if (q_out == q ? q_stride != qw : rope_overlap(q, qn, q_out, qo)) return SDLM_ERR_INVALID_ARG;
-  if (k && (k_out == k ? k_stride != kw : rope_overlap(k, kn, k_out, ko))) return SDLM_ERR_INVALID_ARG;
-  if (k && (rope_overlap(q, qn, k_out, ko) || rope_overlap(k, kn, q_out, qo) || rope_overlap(q_out, qo, k_out, ko)))
+  if (q_out == q ? q_stride != qw : ranges_overlap(q, qn, q_out, qo)) return SDLM_ERR_INVALID_ARG;
+  if (k && (k_out == k ? k_stride != kw : ranges_overlap(k, kn, k_out, ko))) return SDLM_ERR_INVALID_ARG;
+  if (k && (ranges_overlap(q, qn, k_out, ko) || ranges_overlap(k, kn, q_out, qo) || ranges_overlap(q_out, qo, k_out, ko)))
     return SDLM_ERR_INVALID_ARG;
   RopeParams p;
   p.q = static_cast<const __nv_bfloat16*>(q); p.k = static_cast<const __nv_bfloat16*>(k);

@@ -809,6 +809,10 @@ extern "C" sdlm_status sdlm_tree_attn(sdlm_ctx* ctx, int32_t batch, int32_t n, c
   if (!(ctx->scale > 0.0f)) return SDLM_ERR_UNSUPPORTED;
   if (!same_device(ctx)) return SDLM_ERR_INVALID_ARG;
   const sdlm_config& c = ctx->cfg;
+  // rows are read by thread blocks that others, which have their outputs already, do not wait for
+  const size_t row_b = (size_t)batch * n * c.head_dim * 2, q_b = row_b * c.n_q_heads, kv_b = row_b * c.n_kv_heads;
+  if (ranges_overlap(out, q_b, q, q_b) || ranges_overlap(out, q_b, k_tree, kv_b) || ranges_overlap(out, q_b, v_tree, kv_b))
+    return SDLM_ERR_INVALID_ARG;
   const long long rts = ((long long)ctx->group * n + kTreeRows - 1) / kTreeRows;
   const long long positions = (long long)batch * c.n_kv_heads * rts * (kTreeItemCost + (long long)c.max_pages_per_seq + 1);
   if (positions >= (1ll << 30)) return SDLM_ERR_SHAPE;  // they are counted in 32 bits

@@ -98,3 +98,21 @@ def test_captured_pass_follows_its_inputs(filled):
         assert torch.equal(out, filled.tree_attn(q, kt, vt, parent))
         assert torch.equal(token, filled.sample(logits, u)[0])
     g.reset()
+
+
+def test_outputs_in_place_of_inputs_are_refused(filled):
+    q, kt, vt, parent = _tree(3)
+    tok, nxt = torch.zeros_like(parent), torch.ones_like(parent)
+    before = filled.launch_count()
+    wide = torch.zeros((2, *q.shape), dtype=torch.bfloat16, device="cuda").view(-1)[:q.numel() + 64]
+    for call in (lambda: filled.tree_attn(q, kt, vt, parent, out=q),
+                 lambda: filled.tree_attn(wide[64:].view(q.shape), kt, vt, parent, out=wide[:-64].view(q.shape)),
+                 lambda: filled.tree_commit(tok, nxt, parent, kt, vt, out_tokens=nxt),
+                 lambda: filled.tree_commit(tok, nxt, parent, kt, vt, path=parent),
+                 lambda: filled.tree_commit(tok, nxt, parent, kt, vt, out_tokens=(t := torch.zeros_like(tok)), path=t),
+                 lambda: pk.tree_commit_layers([filled], tok, nxt, parent, [kt], [vt], out_tokens=tok)):
+        with pytest.raises(pk.SdlmError) as e:
+            call()
+        assert e.value.code == 1
+    torch.cuda.synchronize()
+    assert filled.launch_count() == before
