@@ -166,7 +166,8 @@ def prepare(case, seed):
         R, V = case["rows"], VOCABS[case["shape"]]
         x = torch.randn((R, V), generator=g, device="cuda") * 2.0
         if case["peak"]:  # a few likely tokens in every row, as a language model has them
-            at = torch.randint(0, V, (R, 40), generator=g, device="cuda")
+            # (one in each fortieth of the vocabulary: of an index drawn twice either value might be left standing)
+            at = torch.randint(0, V // 40, (R, 40), generator=g, device="cuda") + torch.arange(40, device="cuda") * (V // 40)
             up = case["peak"] + 2.0 * torch.randn((R, 40), generator=g, device="cuda")
             x.scatter_(1, at, up)
         if case["banned"]:  # the padding of the vocabulary, and single tokens
