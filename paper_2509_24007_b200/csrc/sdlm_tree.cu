@@ -501,15 +501,19 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attn_kernel(const TreePa
     const uint32_t lane_addr = tmem_base + ((uint32_t)(qd * 32) << 16);
     const uint32_t s_addr = lane_addr + (uint32_t)X * 128, o_addr = lane_addr + O_COL + (uint32_t)X * 128;
     uint32_t cnt = 0, pc = 0;  // items of the group so far, pieces of one tile so far
-    bool ok = true, opening = true;
+    bool ok = true, opening = true, two = false;
     for (; ok && have; have = tree_next(p, walk, n_pos, t)) {
       const int rows_all = min(kTreeRows, p.G * t.s.nodes - t.rt * kTreeRows);
-      const bool two = rows_all > 128;
+      const bool was_two = two;
+      two = rows_all > 128;
       const int row0 = t.rt * kTreeRows + (two ? X * 128 : 0), rows = min(128, p.G * t.s.nodes - row0);
       {
         // Queries into shared memory, swizzled as an MMA operand; rows beyond the end are zero.  Each group stages its
-        // tile, or half of the only one.
-        const int st = tid - 128 - X * 128, q_first = two ? 0 : X * (128 * CH / 2), q_n = two ? CH : CH / 2;
+        // tile, or half of the only one.  Behind a piece with two tiles the first group stages all of the only one: nothing
+        // has joined the groups there, and products of the first, which it has waited for itself, may still read tile 0 when
+        // the second is done.  (A piece with one tile joins them below.)
+        const bool halves = !two && !was_two;
+        const int st = tid - 128 - X * 128, q_first = halves ? X * (128 * CH / 2) : 0, q_n = halves ? CH / 2 : two || X == 0 ? CH : 0;
         const uint32_t qd_s = ptx::smem_u32(q_s + (two ? X * Q_B : 0));
 #pragma unroll 2
         for (int i = 0; i < q_n; ++i) {
