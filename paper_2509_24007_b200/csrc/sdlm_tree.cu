@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attn_kernel(const TreePa
   uint64_t* s_free = s_full + 2;       // [X]: scores in registers
   uint64_t* p_full = s_free + 2;       // [X][buffer]: weights written
   uint64_t* pv_done = p_full + 4;      // [X][buffer]: O += P V of its item, and of those before, complete
-  uint64_t* q_full = pv_done + 4;      // queries staged, the piece before read out of tensor memory
+  uint64_t* q_full = pv_done + 4;      // queries staged, the piece before read out of tensor memory, both issuers there
   uint64_t* l_bar = q_full + 1;        // both groups have left their rows' references and sums in tensor memory
   uint64_t* drain = l_bar + 1;
   TreeStart* start = reinterpret_cast<TreeStart*>(drain + 2);
@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attn_kernel(const TreePa
       ptx::mbar_init(&p_full[s], 4);  // one arrival per softmax warp of the group
       ptx::mbar_init(&pv_done[s], 1);
     }
-    ptx::mbar_init(q_full, 8);
+    ptx::mbar_init(q_full, 10);  // softmax warps and issuers
     ptx::mbar_init(l_bar, 8);
     ptx::mbar_init(&drain[0], 1);
     ptx::mbar_init(&drain[1], 1);
@@ -430,6 +430,9 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attn_kernel(const TreePa
         const bool two = p.G * t.s.nodes - t.rt * kTreeRows > 128;
         const int n_tiles = t.t1 - t.t0, step = two ? 1 : 2, first = two ? 0 : X;
         const uint64_t d_a = d_q + (uint64_t)((two && X ? Q_B : 0) >> 4);
+        // (an issuer arrives too: where its group has no key tile the piece ends without it, and q_full must not be a phase
+        // further when it comes to look)
+        if (lane == 0) ptx::mbar_arrive(q_full);
         ok = ptx::mbar_wait_warp(q_full, pc & 1u, abort);
         ++pc;
         int at_k = 0, at_v = 0;  // tiles of the piece passed so far

@@ -75,3 +75,24 @@ def test_wide_tasks_followed_by_narrow_ones(hq, hk, d, nodes, many, lo, hi):
     _check(t, first, 44.0)
     for _ in range(30):
         assert torch.equal(first, t.attn())
+
+
+@pytest.mark.parametrize("hq,hk,d", [(4, 4, 64), (8, 2, 128)])
+def test_thread_blocks_with_many_tasks_of_one_key_tile(hq, hk, d):
+    """One node on an empty history (its key is the only one: the result is its value, exactly), some 30 tasks a thread
+    block of which the second softmax group and its issuer have no key tile; among them a few of two and three tiles."""
+    lens = [0] * 2000
+    for b in range(0, 2000, 97):
+        lens[b] = 40 + b % 70
+    t = Tree(hq, hk, d, lens, 1, seed=3)
+    want = t.v.repeat_interleave(hq // hk, 2)
+    alone = torch.tensor([x == 0 for x in lens], device="cuda")
+    first = t.attn()
+    assert torch.equal(first[alone], want[alone])
+    for b in range(0, 2000, 97):
+        ref, size = _reference(t, b)
+        # products of size 1: scores are good to d * 2^-24 * 8, the rest as above
+        assert bool(((first[b].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + size * (2.0 ** -7 + 3e-4)).all())
+    for _ in range(50):
+        assert torch.equal(first, t.attn())
+    assert t.sd.device_status()[0] == 0
