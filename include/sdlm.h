@@ -528,8 +528,8 @@ sdlm_status sdlm_tree_attn(sdlm_ctx* ctx, int32_t batch, int32_t n, const int32_
  * nodes in order, -1 behind them; accepted_len[b] = their number (at least 1; 0 without nodes); out_tokens [batch, n]:
  * next_token of the path's nodes, -1 behind them; rows path[b, 0..accepted_len[b]) of k_tree / v_tree
  * [batch, n, Hkv, d] are appended to the cache as sdlm_accept_commit appends its rows.  A sequence that fails
- * commits nothing: accepted_len[b] = -1, its out_tokens are -1.  The outputs must overlap neither each other nor
- * draft_token, next_token and parent.
+ * commits nothing: accepted_len[b] = -1, its out_tokens are -1.  The outputs must overlap neither each other nor an
+ * input (INVALID_ARG).
  * The _layers form commits into several caches (as sdlm_accept_commit_layers; distinct contexts).
  * Uses workspace scratch of the (first) context.
  * Errors: as sdlm_accept_commit(_layers); n <= 64.  Device status: OUT_OF_PAGES, DEVICE_CHECK (also for a slot that

@@ -1315,13 +1315,19 @@ static sdlm_status tree_commit_launch(sdlm_ctx* const* ctxs, int32_t n_layers, i
   sdlm_ctx* c0 = ctxs[0];
   if (!c0) return SDLM_ERR_INVALID_ARG;
   if (batch > c0->cfg.max_batch) return SDLM_ERR_SHAPE;
-  // the outputs are written while tokens and parents of the same tree are still read, in another order
-  const size_t nodes_b = (size_t)batch * n * 4;
-  for (const int32_t* in : {parent, draft_token, next_token})
-    if (ranges_overlap(out_tokens, nodes_b, in, nodes_b) || ranges_overlap(path, nodes_b, in, nodes_b) ||
-        ranges_overlap(accepted_len, (size_t)batch * 4, in, nodes_b))
-      return SDLM_ERR_INVALID_ARG;
-  if (ranges_overlap(path, nodes_b, out_tokens, nodes_b)) return SDLM_ERR_INVALID_ARG;
+  // the outputs are written while the inputs are still read, slot numbers last of all (where the lengths are published)
+  const size_t seqs_b = (size_t)batch * 4, nodes_b = seqs_b * n, rows_b = (size_t)batch * n * c0->cfg.n_kv_heads * c0->cfg.head_dim * 2;
+  const struct { const void* p; size_t bytes; } outs[] = {{accepted_len, seqs_b}, {out_tokens, nodes_b}, {path, nodes_b}},
+      ins[] = {{seq_ids, seqs_b}, {n_nodes, seqs_b}, {parent, nodes_b}, {draft_token, nodes_b}, {next_token, nodes_b}};
+  for (int i = 0; i < 3; ++i) {
+    for (int o = 0; o < i; ++o)
+      if (ranges_overlap(outs[i].p, outs[i].bytes, outs[o].p, outs[o].bytes)) return SDLM_ERR_INVALID_ARG;
+    for (const auto& in : ins)
+      if (in.p && ranges_overlap(outs[i].p, outs[i].bytes, in.p, in.bytes)) return SDLM_ERR_INVALID_ARG;
+    for (int l = 0; l < n_layers; ++l)
+      if (ranges_overlap(outs[i].p, outs[i].bytes, k_tree[l], rows_b) || ranges_overlap(outs[i].p, outs[i].bytes, v_tree[l], rows_b))
+        return SDLM_ERR_INVALID_ARG;
+  }
   CommitLayers* L = new (std::nothrow) CommitLayers;
   if (!L) return SDLM_ERR_CUDA;
   for (int l = 0; l < n_layers; ++l) {

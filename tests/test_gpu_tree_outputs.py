@@ -1,0 +1,76 @@
+"""Outputs of the tree and sampling calls that lie over what is still read, and refusals of the commit one argument at a
+time: each leaves the context and every buffer as they were."""
+import pytest
+import torch
+
+import paper_2509_24007_b200 as pk
+from test_gpu_tree import Tree
+
+pytestmark = pytest.mark.gpu
+
+
+def _refused(sd, call):
+    before = sd.launch_count()
+    with pytest.raises(pk.SdlmError) as e:
+        call()
+    assert e.value.code == 1 and sd.launch_count() == before
+
+
+def _commit_tensors(t):
+    i32 = dict(dtype=torch.int32, device="cuda")
+    return dict(draft_token=torch.zeros((t.B, t.n), **i32), next_token=torch.ones((t.B, t.n), **i32), parent=t.parent,
+                n_nodes=torch.full((t.B,), t.n, **i32), seq_ids=torch.arange(t.B, **i32),
+                accepted_len=torch.full((t.B,), 7, **i32), out_tokens=torch.full((t.B, t.n), 7, **i32),
+                path=torch.full((t.B, t.n), 7, **i32))
+
+
+@pytest.mark.parametrize("layers", [False, True])
+def test_commit_outputs_over_anything_else_are_refused(layers):
+    t = Tree(4, 2, 64, [10, 20, 0], 4, seed=50)
+    a = _commit_tensors(t)
+
+    def call(**kw):
+        kw = {**a, **kw}
+        if layers:
+            return pk.tree_commit_layers([t.sd], k_trees=[kw.pop("k", t.k)], v_trees=[kw.pop("v", t.v)], **kw)
+        return t.sd.tree_commit(k_tree=kw.pop("k", t.k), v_tree=kw.pop("v", t.v), **kw)
+
+    big = torch.full((64,), 7, dtype=torch.int32, device="cuda")   # views into it meet in one element
+    rows, seqs = lambda at: big[at:at + 12].view(3, 4), lambda at: big[at:at + 3]
+    at = lambda name, x: (seqs if a[name].dim() == 1 else rows)(x)
+    size = lambda name: a[name].numel()
+    for out in ("accepted_len", "out_tokens", "path"):
+        for other in a:
+            if other != out:
+                _refused(t.sd, lambda: call(**{out: at(out, 20), other: at(other, 20 + size(out) - 1)}))
+                _refused(t.sd, lambda: call(**{out: at(out, 20), other: at(other, 21 - size(other))}))
+        for rows_of in ("k", "v"):
+            kv = t.k if rows_of == "k" else t.v
+            _refused(t.sd, lambda: call(**{out: kv.view(torch.int32).view(-1)[4:4 + size(out)].view(a[out].shape)}))
+    torch.cuda.synchronize()
+    assert bool((big == 7).all()) and t.sd.kv_tables()["seq_len"].tolist() == [10, 20, 0]
+    assert all(bool((a[x] == 7).all()) for x in ("accepted_len", "out_tokens", "path"))
+    call(accepted_len=seqs(0), out_tokens=rows(3), path=rows(15), seq_ids=seqs(27).copy_(a["seq_ids"]))  # side by side is fine
+    assert seqs(0).tolist() == [1, 1, 1] and t.sd.kv_tables()["seq_len"].tolist() == [11, 21, 1]
+
+
+@pytest.mark.parametrize("kw,code", [(dict(n=65), 2), (dict(batch=3), 2), (dict(batch=0), 1), (dict(n=0), 1)] +
+                         [({x: None}, 1) for x in ("parent", "draft", "next", "k", "v", "acc", "tok", "path")] +
+                         [(dict(k=2), 1), (dict(v=8), 1)])
+def test_one_wrong_argument_of_a_commit_that_is_right(kw, code):
+    t = Tree(4, 2, 64, [10, 20], 4, seed=51)
+    a = _commit_tensors(t)
+    p = dict(parent=a["parent"].data_ptr(), draft=a["draft_token"].data_ptr(), next=a["next_token"].data_ptr(), k=t.k.data_ptr(),
+             v=t.v.data_ptr(), acc=a["accepted_len"].data_ptr(), tok=a["out_tokens"].data_ptr(), path=a["path"].data_ptr())
+
+    def call(batch=2, n=4, **q):
+        q = {**p, **q}
+        return t.sd.lib.sdlm_tree_commit(t.sd.ctx, batch, n, None, None, q["parent"], q["draft"], q["next"], q["k"], q["v"], q["acc"],
+                                         q["tok"], q["path"], torch.cuda.current_stream().cuda_stream)
+
+    before = t.sd.launch_count()
+    assert call(**{x: p[x] + y if x in p and y else y for x, y in kw.items()}) == code
+    torch.cuda.synchronize()
+    assert t.sd.launch_count() == before and t.sd.kv_tables()["seq_len"].tolist() == [10, 20]
+    assert all(bool((a[x] == 7).all()) for x in ("accepted_len", "out_tokens", "path"))
+    assert call() == 0 and a["accepted_len"].tolist() == [1, 1] and t.sd.kv_tables()["seq_len"].tolist() == [11, 21]
