@@ -1388,6 +1388,10 @@ extern "C" sdlm_status sdlm_kv_gather_batch(sdlm_ctx* ctx, int32_t batch, int32_
   if (!same_device(ctx)) return SDLM_ERR_INVALID_ARG;
   const sdlm_config& c = ctx->cfg;
   if (c.n_kv_heads > 65535) return SDLM_ERR_UNSUPPORTED;
+  const size_t rows_b = (size_t)batch * length * c.n_kv_heads * c.head_dim * 2, seqs_b = (size_t)batch * 4;
+  if (ranges_overlap(k_out, rows_b, v_out, rows_b) ||
+      (seq_ids && (ranges_overlap(k_out, rows_b, seq_ids, seqs_b) || ranges_overlap(v_out, rows_b, seq_ids, seqs_b))))
+    return SDLM_ERR_INVALID_ARG;
   const long long most = length < (long long)c.max_pages_per_seq * kPageSize ? length : (long long)c.max_pages_per_seq * kPageSize;
   const int pages = (int)((most + kPageSize - 1) / kPageSize);
   const cudaError_t e = launch_overlapped(kv_gather_batch_kernel, dim3(pages < 4096 ? pages : 4096, c.n_kv_heads, batch), dim3(256),

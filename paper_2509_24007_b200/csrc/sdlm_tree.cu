@@ -818,7 +818,10 @@ extern "C" sdlm_status sdlm_tree_attn(sdlm_ctx* ctx, int32_t batch, int32_t n, c
   const sdlm_config& c = ctx->cfg;
   // rows are read by thread blocks that others, which have their outputs already, do not wait for
   const size_t row_b = (size_t)batch * n * c.head_dim * 2, q_b = row_b * c.n_q_heads, kv_b = row_b * c.n_kv_heads;
-  if (ranges_overlap(out, q_b, q, q_b) || ranges_overlap(out, q_b, k_tree, kv_b) || ranges_overlap(out, q_b, v_tree, kv_b))
+  const size_t seqs_b = (size_t)batch * 4;  // (every role walks the schedule by itself and reads these as it goes)
+  if (ranges_overlap(out, q_b, q, q_b) || ranges_overlap(out, q_b, k_tree, kv_b) || ranges_overlap(out, q_b, v_tree, kv_b) ||
+      ranges_overlap(out, q_b, parent, seqs_b * n) || (n_nodes && ranges_overlap(out, q_b, n_nodes, seqs_b)) ||
+      (seq_ids && ranges_overlap(out, q_b, seq_ids, seqs_b)))
     return SDLM_ERR_INVALID_ARG;
   const long long rts = ((long long)ctx->group * n + kTreeRows - 1) / kTreeRows;
   const long long positions = (long long)batch * c.n_kv_heads * rts * (kTreeItemCost + (long long)c.max_pages_per_seq + 1);

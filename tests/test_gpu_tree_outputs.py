@@ -74,3 +74,25 @@ def test_one_wrong_argument_of_a_commit_that_is_right(kw, code):
     assert t.sd.launch_count() == before and t.sd.kv_tables()["seq_len"].tolist() == [10, 20]
     assert all(bool((a[x] == 7).all()) for x in ("accepted_len", "out_tokens", "path"))
     assert call() == 0 and a["accepted_len"].tolist() == [1, 1] and t.sd.kv_tables()["seq_len"].tolist() == [11, 21]
+
+
+def test_attention_and_gather_outputs_over_index_tensors_are_refused():
+    t = Tree(4, 2, 64, [10, 20, 0], 4, seed=52)
+    ids, nodes = torch.arange(3, dtype=torch.int32, device="cuda"), torch.full((3,), 4, dtype=torch.int32, device="cuda")
+    out = torch.full_like(t.q, 7.0)
+    words = out.view(torch.int32).view(-1)
+    for at in (0, words.numel() - 12):                # the first and the last words of the output
+        w = words[at:at + 12]
+        _refused(t.sd, lambda: t.sd.tree_attn(t.q, t.k, t.v, w.view(3, 4), out=out))
+        _refused(t.sd, lambda: t.sd.tree_attn(t.q, t.k, t.v, t.parent, n_nodes=w[-3:], out=out))
+        _refused(t.sd, lambda: t.sd.tree_attn(t.q, t.k, t.v, t.parent, seq_ids=w[:3], out=out))
+    kv = torch.full((2, 3, 5, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    _refused(t.sd, lambda: t.sd.kv_gather_batch(kv[0], kv[0]))
+    for x in (0, 1):
+        _refused(t.sd, lambda: t.sd.kv_gather_batch(kv[0], kv[1], seq_ids=kv[x].view(torch.int32).view(-1)[-3:]))
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all()) and bool((kv == 7.0).all())
+    t.sd.tree_attn(t.q, t.k, t.v, t.parent, n_nodes=nodes, seq_ids=ids, out=out)
+    t.check(out)
+    t.sd.kv_gather_batch(kv[0], kv[1], seq_ids=ids)   # neighbours are fine
+    assert torch.equal(kv[0, 1], t.kc[1][:5]) and torch.equal(kv[1, 1], t.vc[1][:5])
