@@ -498,7 +498,7 @@ typedef struct sdlm_rope {
  * q [batch, D, n_heads, d] with q_stride elements from one of its batch * D rows to the next (at least n_heads * d, a
  * multiple of 8: the rows may lie inside a stacked q/k/v product); k [batch, D, n_heads2, d] likewise; n_heads2 = 0
  * leaves k out.  q_weight, k_weight: device bf16 [d], either may be NULL.  q_out / k_out: dense rows; either may be
- * its own input when that is dense (in place), no other overlap.  positions: device int32 [batch, D] or NULL for
+ * its own input when that is dense (in place), no other overlap with an input or each other (INVALID_ARG).  positions: device int32 [batch, D] or NULL for
  * 0..D-1 in every sequence; relative != 0, or positions NULL: counted from the length of slot seq_ids[b] (or b) as the
  * tables stand on the stream, else absolute (batch may then exceed max_batch).  Positions may repeat and be negative.
  * Angles are formed in 64 bits; arithmetic fp32 with one rounding to bf16 at the end.

@@ -245,6 +245,10 @@ extern "C" sdlm_status sdlm_qk_norm_rope(sdlm_ctx* ctx, int32_t batch, int32_t D
   if (k && (k_out == k ? k_stride != kw : ranges_overlap(k, kn, k_out, ko))) return SDLM_ERR_INVALID_ARG;
   if (k && (ranges_overlap(q, qn, k_out, ko) || ranges_overlap(k, kn, q_out, qo) || ranges_overlap(q_out, qo, k_out, ko)))
     return SDLM_ERR_INVALID_ARG;
+  const struct { const void* p; size_t bytes; } others[] = {{positions, (size_t)rows * 4}, {counted ? seq_ids : nullptr, (size_t)batch * 4},
+                                                           {q_weight, (size_t)d * 2}, {k_weight, (size_t)d * 2}};
+  for (const auto& in : others)
+    if (in.p && (ranges_overlap(q_out, qo, in.p, in.bytes) || (k && ranges_overlap(k_out, ko, in.p, in.bytes)))) return SDLM_ERR_INVALID_ARG;
   RopeParams p;
   p.q = static_cast<const __nv_bfloat16*>(q); p.k = static_cast<const __nv_bfloat16*>(k);
   p.q_out = static_cast<__nv_bfloat16*>(q_out); p.k_out = static_cast<__nv_bfloat16*>(k_out);

@@ -96,3 +96,23 @@ def test_attention_and_gather_outputs_over_index_tensors_are_refused():
     t.check(out)
     t.sd.kv_gather_batch(kv[0], kv[1], seq_ids=ids)   # neighbours are fine
     assert torch.equal(kv[0, 1], t.kc[1][:5]) and torch.equal(kv[1, 1], t.vc[1][:5])
+
+
+def test_rotary_outputs_over_positions_and_weights_are_refused():
+    t = Tree(4, 2, 64, [10, 20, 0], 4, seed=53)
+    q_out, k_out = torch.full_like(t.q, 7.0), torch.full_like(t.k, 7.0)
+    rope = pk.RopeConfig()
+    for out in (q_out, k_out):
+        flat, words = out.view(-1), out.view(torch.int32).view(-1)
+        call = lambda **kw: t.sd.qk_norm_rope(t.q, t.k, rope, q_out=q_out, k_out=k_out, **kw)
+        _refused(t.sd, lambda: call(positions=words[-12:].view(3, 4)))
+        _refused(t.sd, lambda: call(positions=words[:12].view(3, 4), relative=True))
+        _refused(t.sd, lambda: call(seq_ids=words[-3:]))
+        _refused(t.sd, lambda: call(q_weight=flat[:64]))
+        _refused(t.sd, lambda: call(k_weight=flat[-64:]))
+    _refused(t.sd, lambda: t.sd.qk_norm_rope(t.q, t.k, rope, q_out=q_out, k_out=q_out.view(-1)[:t.k.numel()].view(t.k.shape)))
+    torch.cuda.synchronize()
+    assert bool((q_out == 7.0).all()) and bool((k_out == 7.0).all())
+    a, b = t.sd.qk_norm_rope(t.q, t.k, rope)
+    t.sd.qk_norm_rope(t.q, t.k, rope, q_out=t.q, k_out=t.k)      # in place is fine
+    assert torch.equal(a, t.q) and torch.equal(b, t.k)
