@@ -563,7 +563,9 @@ sdlm_status sdlm_kv_gather_batch(sdlm_ctx* ctx, int32_t batch, int32_t length, c
  * the type's largest finite value; a row with nothing left gives token -1, prob 0, entropy 0, n_kept 0.
  * u float [rows] in [0, 1); temperature, top_p, min_p float [rows], top_k int32 [rows]: device, each of the four may
  * be NULL (1, all, all, all).  token int32, prob / entropy float [rows]: device, required, as sdlm_accept_commit takes
- * them; n_kept int32 [rows] or NULL.  logits: aligned to its type (16-byte rows are read faster).
+ * them; n_kept int32 [rows] or NULL.  Outputs must overlap neither each other nor logits; an output may be one of the five
+ * arrays above (it is then replaced row for row), but not overlap it otherwise (INVALID_ARG).  logits: aligned to its type
+ * (16-byte rows are read faster).
  * Weights are formed in 64 bits and summed exactly: results do not depend on timing.  No workspace scratch.
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (vocab > 262144), CUDA. */
 typedef enum sdlm_logit_type { SDLM_LOGITS_BF16 = 0, SDLM_LOGITS_F32 = 1 } sdlm_logit_type;

@@ -1022,6 +1022,19 @@ extern "C" sdlm_status sdlm_sample(sdlm_ctx* ctx, int32_t rows, int32_t vocab, s
   if (vocab > kSampleMaxVocab) return SDLM_ERR_UNSUPPORTED;  // sums of weights in 64 bits; a slice in shared memory
   if (rows > (1 << 27)) return SDLM_ERR_SHAPE;
   if (!same_device(ctx)) return SDLM_ERR_INVALID_ARG;
+  // Outputs must not lie over logits or each other; over the rows' parameters only row for row (a row's thread blocks have
+  // all read theirs when its results are written, other rows' have not).
+  const size_t per_row = (size_t)rows * 4, logits_b = ((size_t)(rows - 1) * row_stride + vocab) * (f32 ? 4 : 2);
+  const void* const outs[] = {token, prob, entropy, n_kept};
+  const void* const ins[] = {u, temperature, top_k, top_p, min_p};
+  for (int i = 0; i < 4; ++i) {
+    if (!outs[i]) continue;
+    if (ranges_overlap(outs[i], per_row, logits, logits_b)) return SDLM_ERR_INVALID_ARG;
+    for (int o = 0; o < i; ++o)
+      if (ranges_overlap(outs[i], per_row, outs[o], per_row)) return SDLM_ERR_INVALID_ARG;
+    for (const void* in : ins)
+      if (in && in != outs[i] && ranges_overlap(outs[i], per_row, in, per_row)) return SDLM_ERR_INVALID_ARG;
+  }
   SampleParams p;
   p.logits = logits; p.ld = row_stride; p.u = u; p.temperature = temperature; p.top_k = top_k; p.top_p = top_p; p.min_p = min_p;
   p.token = token; p.prob = prob; p.entropy = entropy; p.kept = n_kept;

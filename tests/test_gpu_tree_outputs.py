@@ -116,3 +116,35 @@ def test_rotary_outputs_over_positions_and_weights_are_refused():
     a, b = t.sd.qk_norm_rope(t.q, t.k, rope)
     t.sd.qk_norm_rope(t.q, t.k, rope, q_out=t.q, k_out=t.k)      # in place is fine
     assert torch.equal(a, t.q) and torch.equal(b, t.k)
+
+
+def test_sampling_outputs_over_logits_parameters_and_each_other():
+    sd = pk.Sdlm(pk.SdlmConfig(2, 1, 64, 64, 64, 4, 4, 4, max_block=8))
+    R, V = 9, 5000
+    g = torch.Generator("cuda").manual_seed(54)
+    logits = torch.randn((R, V), device="cuda", generator=g) * 3
+    f = {x: torch.rand(R, device="cuda", generator=g) for x in ("u", "temperature", "top_p", "min_p")}
+    f["min_p"] *= 0.1
+    f["top_k"] = torch.arange(R, dtype=torch.int32, device="cuda") * 30
+    made = lambda: dict(token=torch.full((R,), 7, dtype=torch.int32, device="cuda"), prob=torch.full((R,), 7.0, device="cuda"),
+                        entropy=torch.full((R,), 7.0, device="cuda"), n_kept=torch.full((R,), 7, dtype=torch.int32, device="cuda"))
+    call = lambda **kw: sd.sample(logits, **{**f, **made(), **kw})
+    want = call()
+    big = torch.zeros(40, device="cuda")
+    as_ = lambda name, x: x.view(torch.int32) if name in ("token", "n_kept", "top_k") else x
+    for out in made():
+        at = lambda i: as_(out, big[i:i + R])
+        _refused(sd, lambda: call(**{out: as_(out, logits.view(-1)[:R])}))
+        _refused(sd, lambda: call(**{out: as_(out, logits.view(-1)[-R:])}))
+        for other in (*f, *(x for x in made() if x != out)):
+            _refused(sd, lambda: call(**{out: at(10), other: as_(other, big[10 + R - 1:10 + 2 * R - 1])}))
+            _refused(sd, lambda: call(**{out: at(10), other: as_(other, big[11 - R:11])}))
+        for other in (x for x in made() if x != out):
+            _refused(sd, lambda: call(**{out: at(10), other: as_(other, big[10:10 + R])}))
+    torch.cuda.synchronize()
+    assert bool((big == 0).all())
+    # in place of a parameter, row for row
+    for out, param in (("token", "top_k"), ("prob", "u"), ("entropy", "temperature"), ("n_kept", "top_k"), ("prob", "top_p"), ("prob", "min_p")):
+        same = f[param].clone()
+        got = call(**{param: same, out: same})
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
