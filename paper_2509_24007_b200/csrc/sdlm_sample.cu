@@ -681,15 +681,11 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleP
   s.bin_scale = (float)kSampleBins / (20.0f * fminf(fmaxf(greedy ? 1.0f : T, 1e-30f), 1e30f));
   SampleCut cut{-INFINITY, 0u};
   const bool by_k = k > 1 && k < p.V, by_p = top_p < 1.0f;
-  // 0: nothing to find, 1: the first token alone, 2: thresholds.  Opaque to the compiler: nvcc 12.9 takes the branch for 2
-  // out when it can see through the condition, and the filters then keep everything (the tests show it).
-  int mode = greedy || k == 1 ? 1 : by_k || by_p ? 2 : 0;
-  asm volatile("" : "+r"(mode));
   SampleSums own{0, 0.0, 0, 0};  // this thread block's kept tokens, once known
   bool summed = false, few = false;
-  if (mode == 1) {
+  if (greedy || k == 1) {  // the first token alone
     cut = SampleCut{mx, 1u};
-  } else if (mode == 2) {
+  } else if (by_k || by_p) {
     const double p64 = fmax((double)top_p, 0.0);
     s.find_bins(by_k, k, by_p);
     const int b_k = sh->b_k;
