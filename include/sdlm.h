@@ -513,7 +513,7 @@ sdlm_status sdlm_qk_norm_rope(sdlm_ctx* ctx, int32_t batch, int32_t D, const int
  *   nodes on the path of node j and j itself.
  * q, out [batch, n, Hq, d]; k_tree / v_tree [batch, n, Hkv, d]: device bf16; parent device int32 [batch, n].
  * 1 <= n <= 64; any Hq/Hkv; max_block does not limit n.  n = 1 is attention of a single token.  Slots may repeat.
- * K and V of the tree's nodes have to be finite; out must not overlap an input.  fp32 scores, sums and accumulation, weights rounded to bf16 before
+ * An infinity or NaN in K or V reaches the rows that see its token and no others; out must not overlap an input.  fp32 scores, sums and accumulation, weights rounded to bf16 before
  * they meet V, bf16 output; results do not depend on timing.  The cache is not modified.
  * Uses workspace scratch: calls on one context must not overlap on the GPU.
  * Errors: INVALID_ARG, SHAPE (batch, n, or a schedule beyond 32 bits), UNSUPPORTED (softmax_scale not positive), CUDA. */

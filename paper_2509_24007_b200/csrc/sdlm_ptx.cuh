@@ -554,11 +554,18 @@ __device__ __forceinline__ float2 add2_f2(float2 a, float2 b) {
 // 2^t for two arguments t <= 2^7 on the FMA and integer pipes instead of the special-function unit, which is
 // the narrowest pipe of the softmax: t = n + f with n = round(t), |f| <= 1/2; 2^f from a cubic fitted for the
 // smallest largest relative error on that interval (7.5e-5, a twenty-fifth of the bf16 rounding that follows);
-// n goes into the exponent field.  Arguments below -125 give 2^-125 times the cubic (weights that small add nothing).
+// n goes into the exponent field.  Arguments below -125 give 2^-125 times the cubic (weights that small add nothing);
+// so does NaN, or with KEEP_NAN something of 2^127 or more (infinity as bf16).
+template <bool KEEP_NAN = false>
 __device__ __forceinline__ float2 exp2_poly2(float2 t) {
   const float kMagic = 12582912.f;  // 1.5 * 2^23: adding it leaves round(t) in the low mantissa bits
-  t.x = fmaxf(t.x, -125.f);
-  t.y = fmaxf(t.y, -125.f);
+  if (KEEP_NAN) {
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(t.x) : "f"(-125.f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(t.y) : "f"(-125.f));
+  } else {
+    t.x = fmaxf(t.x, -125.f);
+    t.y = fmaxf(t.y, -125.f);
+  }
   const float2 r = add2_f2(t, make_float2(kMagic, kMagic));
   const float2 n = add2_f2(r, make_float2(-kMagic, -kMagic));
   const float2 f = fma2_f2(n, make_float2(-1.f, -1.f), t);

@@ -30,6 +30,9 @@
 #include "sdlm_internal.h"
 #include "sdlm_ptx.cuh"
 
+#include <float.h>
+#include <math.h>
+
 namespace sdlm {
 
 constexpr int kTreeThreads = 384;
@@ -79,7 +82,7 @@ __device__ __forceinline__ void tree_umma_ts(uint32_t d_tmem, uint32_t a_tmem, u
       : "memory");
 }
 
-// Largest of a thread's 64 scores (four chains); with EDGE only over the keys whose bit is set.
+// Largest of a thread's 64 scores (four chains), NaN left out; with EDGE only over the keys whose bit is set.
 template <bool EDGE>
 __device__ __forceinline__ float tree_row_max(const uint32_t (&x)[64], uint32_t lo, uint32_t hi) {
   float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -113,7 +116,7 @@ __device__ __forceinline__ float tree_weights(const uint32_t (&x)[64], uint32_t 
       const float2 t = ptx::fma2_f2(make_float2(__uint_as_float(x[c * 32 + i]), __uint_as_float(x[c * 32 + i + 1])), scale2, neg_ref2);
       float2 w;
       if (((i >> 1) & 3) == 1) {
-        w = ptx::exp2_poly2(t);
+        w = ptx::exp2_poly2<true>(t);
       } else {
         w.x = ptx::ex2(t.x);
         w.y = ptx::ex2(t.y);
@@ -135,6 +138,50 @@ __device__ __forceinline__ void tree_status(const TreeParams& p, int code, int s
   if (atomicCAS(&p.hdr->status[0], 0, code) == 0) {
     p.hdr->status[1] = slot;
     p.hdr->status[2] = detail;
+  }
+}
+
+// Values of the tree's nodes that are not finite: a weight of zero times one is NaN in the product, which covers all nodes
+// for all rows.  They are zero in the tile, and are added to the rows that see their node once those are written (a weight
+// above zero times an infinity or NaN is one).
+__device__ __forceinline__ uint32_t tree_largest(uint32_t most, const uint4& v) {  // of |bf16| pairs, NaN above all
+  __nv_bfloat162 m = *reinterpret_cast<__nv_bfloat162*>(&most);
+  const __nv_bfloat162* b = reinterpret_cast<const __nv_bfloat162*>(&v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = __hmax2_nan(m, __habs2(b[i]));
+  return *reinterpret_cast<uint32_t*>(&m);
+}
+__device__ __forceinline__ bool tree_spoiled(uint32_t pair) {  // one of two bf16 is not finite
+  return (pair & 0x7f80u) == 0x7f80u || (pair & 0x7f800000u) == 0x7f800000u;
+}
+// Puts zero in their place in the V^T tile that a warp has written (whole warps); the nodes that have any.
+template <int HD>
+__device__ __noinline__ uint64_t tree_clean(uint8_t* tile, const __nv_bfloat16* v, size_t stride, int nodes) {
+  const int lane = threadIdx.x & 31;
+  uint32_t lo = 0, hi = 0;
+  __syncwarp();
+  for (int i = lane; i < nodes * HD; i += 32) {
+    const int key = i / HD, col = i % HD;
+    if (isfinite(__bfloat162float(v[key * stride + col]))) continue;
+    *reinterpret_cast<uint16_t*>(tile + col * 128 + (((key >> 3) ^ (col & 7)) << 4) + (key & 7) * 2) = 0;
+    if (key < 32) lo |= 1u << key; else hi |= 1u << (key - 32);
+  }
+  __syncwarp();
+  lo = __reduce_or_sync(0xffffffffu, lo);
+  hi = __reduce_or_sync(0xffffffffu, hi);
+  return (uint64_t)hi << 32 | lo;
+}
+template <typename T>  // columns [first, last) of a row written by this thread; v: the sequence's values of its KV head
+__device__ __noinline__ void tree_add_spoiled(T* row, int first, int last, const __nv_bfloat16* v, size_t stride, const int32_t* parent,
+                                              int node, uint64_t spoiled) {
+  for (int i = node; i >= 0;) {
+    if (spoiled >> i & 1u)
+      for (int c = first; c < last; ++c) {
+        const float x = __bfloat162float(v[i * stride + c]);
+        if (!isfinite(x)) row[c] = (T)((float)row[c] + x);
+      }
+    const int up = parent[i];
+    i = up < i ? up : -1;
   }
 }
 
@@ -225,7 +272,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attn_kernel(const TreePa
   uint64_t* q_full = pv_done + 4;      // queries staged, the piece before read out of tensor memory, both issuers there
   uint64_t* l_bar = q_full + 1;        // both groups have left their rows' references and sums in tensor memory
   uint64_t* drain = l_bar + 1;
-  TreeStart* start = reinterpret_cast<TreeStart*>(drain + 2);
+  uint64_t* spoiled = drain + 2;       // [16] by piece: nodes with values that are not finite
+  TreeStart* start = reinterpret_cast<TreeStart*>(spoiled + 16);
   int* warp_sum = reinterpret_cast<int*>(start + 1);  // [12]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(warp_sum + 12);
   volatile int* abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -333,9 +381,9 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attn_kernel(const TreePa
       uint64_t* freed = v_part ? v_free : k_free;
       bool ok = true;
       int slot = 0, used = 0;
-      uint32_t ph = 1;  // phase of the slot's use before
+      uint32_t ph = 1, n_piece = 0;  // phase of the slot's use before
       if (have) asm volatile("bar.sync 1, 320;" ::: "memory");  // the softmax warps have asked for their first queries
-      for (; ok && have; have = tree_next(p, walk, n_pos, t)) {
+      for (; ok && have; have = tree_next(p, walk, n_pos, t), ++n_piece) {
         const int cached = t.s.tiles - 1, end = min(t.t1, cached);
         const int32_t* pages = p.page_table + (size_t)t.s.slot * p.mpps;
         const size_t head_off = (size_t)t.hk * 2 * kv_tile_elems(HD);
@@ -373,6 +421,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attn_kernel(const TreePa
               ptx::cp_async_commit();
               ptx::cp_async_wait<0>();
             } else {  // values: blocks of eight keys by eight columns, transposed in registers
+              uint32_t most = 0;
 #pragma unroll 2
               for (int i = 0; i < CH / 4; ++i) {
                 const int blk = lane + i * 32, kb = blk / CH, c = blk % CH;
@@ -382,6 +431,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attn_kernel(const TreePa
                   v[e] = make_uint4(0, 0, 0, 0);
                   if (kb * 8 + e < t.s.nodes) v[e] = *(reinterpret_cast<const uint4*>(src + (kb * 8 + e) * stride) + c);
                 }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) most = tree_largest(most, v[e]);
 #pragma unroll
                 for (int col = 0; col < 8; ++col) {
                   uint32_t o[4];
@@ -394,6 +445,11 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attn_kernel(const TreePa
                   *reinterpret_cast<uint4*>(tile + (c * 8 + col) * 128 + ((kb ^ col) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
                 }
               }
+              // Read once the products of this tile are complete.  The ring lets this warp run at most 8 pieces ahead of the
+              // issuers, which stay in a piece until all its rows are written.
+              uint64_t bad = 0;
+              if (__any_sync(0xffffffffu, tree_spoiled(most))) bad = tree_clean<HD>(tile, src, stride, t.s.nodes);
+              if (lane == 0) spoiled[n_piece & 15u] = bad;
             }
             ptx::fence_proxy_async();
             __syncwarp();
@@ -503,9 +559,9 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attn_kernel(const TreePa
     const int X = (warp - 4) >> 2, qd = warp & 3, row = qd * 32 + lane;
     const uint32_t lane_addr = tmem_base + ((uint32_t)(qd * 32) << 16);
     const uint32_t s_addr = lane_addr + (uint32_t)X * 128, o_addr = lane_addr + O_COL + (uint32_t)X * 128;
-    uint32_t cnt = 0, pc = 0;  // items of the group so far, pieces of one tile so far
+    uint32_t cnt = 0, pc = 0, n_piece = 0;  // items of the group so far, pieces of one tile so far, pieces
     bool ok = true, opening = true, two = false;
-    for (; ok && have; have = tree_next(p, walk, n_pos, t)) {
+    for (; ok && have; have = tree_next(p, walk, n_pos, t), ++n_piece) {
       const int rows_all = min(kTreeRows, p.G * t.s.nodes - t.rt * kTreeRows);
       const bool was_two = two;
       two = rows_all > 128;
@@ -602,6 +658,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attn_kernel(const TreePa
         const float neg_ref = m_ref == -INFINITY ? 0.f : -m_ref;
         const uint32_t p_addr = s_addr + 64 + buf * 32;
         l += edge ? tree_weights<true>(x, p_addr, p.scale_log2, neg_ref, lo, hi) : tree_weights<false>(x, p_addr, p.scale_log2, neg_ref, 0, 0);
+        if (mx == INFINITY) l = NAN;  // (the cubic would give the quotient of two infinities a weight)
         ptx::tmem_st_wait();
         ptx::tc_fence_before();
         __syncwarp();
@@ -675,6 +732,13 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attn_kernel(const TreePa
             }
           }
         }
+        if (t.t1 == t.s.tiles && row < rows && spoiled[n_piece & 15u]) {
+          const size_t stride = (size_t)p.Hkv * HD;
+          const __nv_bfloat16* v = p.v_tree + ((size_t)t.b * p.n * p.Hkv + t.hk) * HD;
+          const int32_t* parent = p.parent + (size_t)t.b * p.n;
+          if (all) tree_add_spoiled(out_row, c_first * 16, c_last * 16, v, stride, parent, my_node, spoiled[n_piece & 15u]);
+          else tree_add_spoiled(reinterpret_cast<float*>(part), c_first * 16, c_last * 16, v, stride, parent, my_node, spoiled[n_piece & 15u]);
+        }
       }
     }
     if (!ok && lane == 0) tree_status(p, SDLM_ERR_TIMEOUT, -2, 13);
@@ -736,7 +800,9 @@ __global__ void __launch_bounds__(kTreeMergeThreads) tree_merge_kernel(const Tre
     for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
 #pragma unroll
     for (int i = 0; i < KL; ++i) {
-      w[i] = ml[i].x == -INFINITY ? 0.f : exp2f(ml[i].x - M);  // (a piece in which the row saw nothing adds nothing)
+      w[i] = exp2f(ml[i].x - M);
+      if (w[i] < FLT_MIN) w[i] = FLT_MIN;     // nothing beside the others, but an infinity stays one
+      if (ml[i].x == -INFINITY) w[i] = 0.f;   // a piece in which the row saw nothing adds nothing
       L = fmaf(w[i], ml[i].y, L);
     }
 #pragma unroll
@@ -780,8 +846,8 @@ __global__ void __launch_bounds__(kTreeMergeThreads) tree_merge_kernel(const Tre
 template <int HD>
 static cudaError_t tree_launch(sdlm_ctx* ctx, TreeParams& p, cudaStream_t st) {
   const int tile_b = HD * 128;
-  // alignment slack, the tiles' queries, 17 barriers, the schedule, flags; two barriers per ring slot
-  const int fixed = 1024 + p.q_tiles * (HD / 64) * 128 * 128 + 17 * 8 + (int)sizeof(TreeStart) + 12 * 4 + 16;
+  // alignment slack, the tiles' queries, 17 barriers, 16 sets of nodes, the schedule, flags; two barriers per ring slot
+  const int fixed = 1024 + p.q_tiles * (HD / 64) * 128 * 128 + (17 + 16) * 8 + (int)sizeof(TreeStart) + 12 * 4 + 16;
   const int slots = (kTreeSmemLimit - fixed) / (tile_b + 16);
   if (slots < 4) return cudaErrorLaunchOutOfResources;
   p.n_k = p.n_v = slots / 2 > 8 ? 8 : slots / 2;
