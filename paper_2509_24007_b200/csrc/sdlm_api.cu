@@ -515,7 +515,6 @@ using namespace sdlm;
 // ---------------------------------------------------------------------------------------------
 // C ABI
 // ---------------------------------------------------------------------------------------------
-static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 // RESTORE and IMPORT write the exported region from here on: free_head, free_tail (and the two tickets,
 // zero between launches), then the tables.  The status words in front of them stay as they are.
 constexpr size_t kStateOffset = offsetof(DevHeader, free_head);

@@ -296,12 +296,6 @@ struct Ring {
   }
 };
 
-__device__ __forceinline__ uint64_t attn_smem_desc(uint32_t saddr) {
-  // K-major operand, 128-byte swizzle, 8-row groups 1024 bytes apart; descriptor version 1 (sm_100)
-  return (uint64_t)((saddr & 0x3FFFF) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) |
-         ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
-
 
 constexpr int kIntMin = -2147483647 - 1;
 // Order-preserving map float -> int (for integer warp reductions of float maxima) and back.
@@ -583,7 +577,7 @@ __global__ void __launch_bounds__(attn_threads(NQ), 1) block_attn_umma_kernel(co
     // The whole warp walks the items and waits; one elected lane issues (see ptx::elect_one).
     {
       const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NQ >> 3) << 17) | ((128u >> 4) << 24);
-      const uint64_t d_q = attn_smem_desc(ptx::smem_u32(q_s)), d_st = attn_smem_desc(ptx::smem_u32(stages));
+      const uint64_t d_q = ptx::umma_smem_desc(ptx::smem_u32(q_s)), d_st = ptx::umma_smem_desc(ptx::smem_u32(stages));
       ItemWalk w = w0;  // the walk behind the first item, which every thread has worked out already
       Item it = i0;
       Ring ring{0, 0};
@@ -626,7 +620,7 @@ __global__ void __launch_bounds__(attn_threads(NQ), 1) block_attn_umma_kernel(co
     // ---------------------------------------------------------------- O^T += V^T P^T issuer
     {
       const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NQ >> 3) << 17) | ((128u >> 4) << 24);
-      const uint64_t d_p = attn_smem_desc(ptx::smem_u32(p_s)), d_st = attn_smem_desc(ptx::smem_u32(stages));
+      const uint64_t d_p = ptx::umma_smem_desc(ptx::smem_u32(p_s)), d_st = ptx::umma_smem_desc(ptx::smem_u32(stages));
       ItemWalk w = w0;  // the walk behind the first item, which every thread has worked out already
       Item it = i0;
       Ring ring{0, 0};

@@ -70,22 +70,6 @@ struct CausalParams {
 constexpr int kCausalThreads = 640;
 constexpr float kCausalRebase = 8.0f;  // log2 units a score may exceed its row reference by
 
-__device__ __forceinline__ uint64_t causal_smem_desc(uint32_t saddr) {
-  // K-major operand, 128-byte swizzle, 8-row groups 1024 bytes apart; descriptor version 1 (sm_100)
-  return (uint64_t)((saddr & 0x3FFFF) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) |
-         ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
-
-// D (tensor memory) = or += A (tensor memory: 128 lanes, two bf16 of consecutive k per 32-bit column) * B (shared memory)
-__device__ __forceinline__ void causal_umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-
 // Largest of a thread's 64 scores; with EDGE only over the keys k0 + i < my_keys the row sees.
 template <bool EDGE>
 __device__ __forceinline__ float causal_row_max(const uint32_t (&x)[64], int k0, int my_keys) {
@@ -312,8 +296,8 @@ __global__ void __launch_bounds__(kCausalThreads, 1) causal_attn_umma_kernel(con
       // was read from.  The whole warp runs the loop and the waits; one elected lane issues (see ptx::elect_one).
       const uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
       const uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(HD >> 3) << 17) | ((128u >> 4) << 24);
-      const uint64_t d_q = causal_smem_desc(ptx::smem_u32(q_s));
-      const uint64_t d_kr = causal_smem_desc(ptx::smem_u32(k_ring)), d_vr = causal_smem_desc(ptx::smem_u32(v_ring));
+      const uint64_t d_q = ptx::umma_smem_desc(ptx::smem_u32(q_s));
+      const uint64_t d_kr = ptx::umma_smem_desc(ptx::smem_u32(k_ring)), d_vr = ptx::umma_smem_desc(ptx::smem_u32(v_ring));
       bool ok = true;
       CAUSAL_PH_DECL;
       CAUSAL_T(i_start);
@@ -334,7 +318,7 @@ __global__ void __launch_bounds__(kCausalThreads, 1) causal_attn_umma_kernel(con
               for (int j = 0; j < tiles; ++j)
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                  causal_umma_ts(tmem_base + O_COL + x * 128, tmem_base + x * 128 + j * 64 + k * 8,
+                  ptx::umma_bf16_ts(tmem_base + O_COL + x * 128, tmem_base + x * 128 + j * 64 + k * 8,
                                  d_v + (uint64_t)((j * VT_B + k * 32) >> 4), idesc_o, (gv | j | k) ? 1u : 0u);
               if (x == n_heads - 1) ptx::umma_commit(&v_free[vs]);
             }

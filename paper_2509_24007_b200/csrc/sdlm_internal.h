@@ -171,6 +171,8 @@ inline cudaError_t launch_overlapped_cluster(void (*kernel)(KArgs...), dim3 grid
   return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
 }
 
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
 // Whether [a, a + an) and [b, b + bn) (bytes) share any.
 inline bool ranges_overlap(const void* a, size_t an, const void* b, size_t bn) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);

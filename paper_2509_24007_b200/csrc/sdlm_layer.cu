@@ -103,8 +103,6 @@ __global__ void __launch_bounds__(256) swiglu_kernel(const __nv_bfloat16* gate_u
   }
 }
 
-static inline bool a16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 cudaError_t launch_rmsnorm(sdlm_ctx* ctx, int rows, int H, const void* x, const void* weight, float eps, void* out,
                            cudaStream_t st) {
   const cudaError_t e = launch_overlapped(rmsnorm_kernel, dim3(rows), dim3(128), 0, st, static_cast<const __nv_bfloat16*>(x),
@@ -121,7 +119,7 @@ using namespace sdlm;
 extern "C" sdlm_status sdlm_linear(sdlm_ctx* ctx, int32_t rows, int32_t K, int32_t N, const void* x, const void* w,
                                    const void* bias, const void* residual, void* out, void* stream) {
   if (!ctx || !x || !w || !out || rows < 1 || K < 8 || N < 16) return SDLM_ERR_INVALID_ARG;
-  if (!a16(x) || !a16(w) || !a16(out) || (bias && !a16(bias)) || (residual && !a16(residual))) return SDLM_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(w) || !aligned16(out) || (bias && !aligned16(bias)) || (residual && !aligned16(residual))) return SDLM_ERR_INVALID_ARG;
   if (K % 8 || N % 16) return SDLM_ERR_UNSUPPORTED;
   return launch_linear(ctx, rows, K, N, x, w, bias, residual, out, static_cast<cudaStream_t>(stream));
 }
@@ -131,7 +129,7 @@ extern "C" sdlm_status sdlm_linear3(sdlm_ctx* ctx, int32_t rows, int32_t K, int3
                                     void* stream) {
   if (!ctx || !x || !w || !out1 || !out2 || !out3 || rows < 1 || K < 8 || N1 < 16 || N2 < 16 || N3 < 16)
     return SDLM_ERR_INVALID_ARG;
-  if (!a16(x) || !a16(w) || !a16(out1) || !a16(out2) || !a16(out3) || (bias && !a16(bias))) return SDLM_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(w) || !aligned16(out1) || !aligned16(out2) || !aligned16(out3) || (bias && !aligned16(bias))) return SDLM_ERR_INVALID_ARG;
   if (K % 8 || N1 % 16 || N2 % 16 || N3 % 16) return SDLM_ERR_UNSUPPORTED;
   return launch_linear(ctx, rows, K, N1 + N2 + N3, x, w, bias, nullptr, out1, static_cast<cudaStream_t>(stream), N1,
                        N1 + N2, out2, out3);
@@ -140,7 +138,7 @@ extern "C" sdlm_status sdlm_linear3(sdlm_ctx* ctx, int32_t rows, int32_t K, int3
 extern "C" sdlm_status sdlm_linear_swiglu(sdlm_ctx* ctx, int32_t rows, int32_t K, int32_t I, const void* x,
                                           const void* w_interleaved, void* out, void* stream) {
   if (!ctx || !x || !w_interleaved || !out || rows < 1 || K < 8 || I < 8) return SDLM_ERR_INVALID_ARG;
-  if (!a16(x) || !a16(w_interleaved) || !a16(out)) return SDLM_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(w_interleaved) || !aligned16(out)) return SDLM_ERR_INVALID_ARG;
   if (K % 8 || I % 8) return SDLM_ERR_UNSUPPORTED;
   return launch_linear(ctx, rows, K, 2 * I, x, w_interleaved, nullptr, nullptr, out, static_cast<cudaStream_t>(stream), 0, 0,
                        nullptr, nullptr, 1);
@@ -149,7 +147,7 @@ extern "C" sdlm_status sdlm_linear_swiglu(sdlm_ctx* ctx, int32_t rows, int32_t K
 extern "C" sdlm_status sdlm_rmsnorm(sdlm_ctx* ctx, int32_t rows, int32_t H, const void* x, const void* weight, float eps,
                                     void* out, void* stream) {
   if (!ctx || !x || !weight || !out || rows < 1 || H < 8 || !(eps >= 0.f)) return SDLM_ERR_INVALID_ARG;
-  if (!a16(x) || !a16(weight) || !a16(out)) return SDLM_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(weight) || !aligned16(out)) return SDLM_ERR_INVALID_ARG;
   if (H % 8) return SDLM_ERR_UNSUPPORTED;
   return launch_rmsnorm(ctx, rows, H, x, weight, eps, out, static_cast<cudaStream_t>(stream)) == cudaSuccess ? SDLM_OK
                                                                                                              : SDLM_ERR_CUDA;
@@ -160,8 +158,8 @@ extern "C" sdlm_status sdlm_linear_rmsnorm(sdlm_ctx* ctx, int32_t rows, int32_t 
                                            float eps, void* norm_out, void* stream) {
   if (!ctx || !x || !w || !out || !norm_weight || !norm_out || rows < 1 || K < 8 || N < 16 || !(eps >= 0.f))
     return SDLM_ERR_INVALID_ARG;
-  if (!a16(x) || !a16(w) || !a16(out) || !a16(norm_weight) || !a16(norm_out) || (bias && !a16(bias)) ||
-      (residual && !a16(residual)))
+  if (!aligned16(x) || !aligned16(w) || !aligned16(out) || !aligned16(norm_weight) || !aligned16(norm_out) || (bias && !aligned16(bias)) ||
+      (residual && !aligned16(residual)))
     return SDLM_ERR_INVALID_ARG;
   if (K % 8 || N % 16) return SDLM_ERR_UNSUPPORTED;
   const LinNorm norm{norm_weight, eps, norm_out};
@@ -239,7 +237,7 @@ extern "C" sdlm_status sdlm_linear3_rope(sdlm_ctx* ctx, int32_t batch, int32_t D
                                          void* q, void* k, void* v, float theta, void* stream) {
   if (!ctx || !x || !w || !q || !k || !v || batch < 1 || D < 1 || K < 8 || n_heads < 1 || n_heads2 < 1 || !(theta > 1.f))
     return SDLM_ERR_INVALID_ARG;
-  if (!a16(x) || !a16(w) || !a16(q) || !a16(k) || !a16(v) || (bias && !a16(bias))) return SDLM_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(w) || !aligned16(q) || !aligned16(k) || !aligned16(v) || (bias && !aligned16(bias))) return SDLM_ERR_INVALID_ARG;
   if (batch > ctx->cfg.max_batch) return SDLM_ERR_SHAPE;
   const int d = ctx->cfg.head_dim;
   if (K % 8 || d % 16) return SDLM_ERR_UNSUPPORTED;
@@ -251,7 +249,7 @@ extern "C" sdlm_status sdlm_linear3_rope(sdlm_ctx* ctx, int32_t batch, int32_t D
 
 extern "C" sdlm_status sdlm_swiglu(sdlm_ctx* ctx, int32_t rows, int32_t I, const void* gate_up, void* out, void* stream) {
   if (!ctx || !gate_up || !out || rows < 1 || I < 8) return SDLM_ERR_INVALID_ARG;
-  if (!a16(gate_up) || !a16(out)) return SDLM_ERR_INVALID_ARG;
+  if (!aligned16(gate_up) || !aligned16(out)) return SDLM_ERR_INVALID_ARG;
   if (I % 8) return SDLM_ERR_UNSUPPORTED;
   const size_t total = (size_t)rows * (I / 8);
   const int blocks = (int)((total + 255) / 256 < 1184 ? (total + 255) / 256 : 1184);

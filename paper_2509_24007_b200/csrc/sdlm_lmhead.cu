@@ -89,12 +89,6 @@ constexpr int kUmmaThreads = 192;  // warp 0 producer, warp 1 MMA + TMEM owner, 
 constexpr int kBK = 64;            // K elements per stage: one 128-byte swizzle row
 constexpr int kATileBytes = 128 * kBK * 2;
 
-__device__ __forceinline__ uint64_t umma_smem_desc(uint32_t saddr) {
-  // K-major, 128-byte swizzle: 8-row groups 1024 bytes apart; descriptor version 1 (sm_100)
-  return (uint64_t)((saddr & 0x3FFFF) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) |
-         ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
-
 __device__ __forceinline__ void lm_timeout(DevHeader* hdr, int where) {
   if (atomicCAS(&hdr->status[0], 0, (int)SDLM_ERR_TIMEOUT) == 0) {
     hdr->status[1] = -2;
@@ -342,7 +336,7 @@ __global__ void __launch_bounds__(kUmmaThreads, 1)
     {
       // instruction descriptor: D fp32, A and B bf16, both K-major, N = bn, M = 128
       const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(p.bn >> 3) << 17) | ((128u >> 4) << 24);
-      const uint64_t d_smem = umma_smem_desc(ptx::smem_u32(smem));  // byte offsets / 16 are added to its address field
+      const uint64_t d_smem = ptx::umma_smem_desc(ptx::smem_u32(smem));  // byte offsets / 16 are added to its address field
       uint32_t it = 0;
       bool ok = true;
       for (int t = 0; t < n_tiles && ok; ++t) {
@@ -574,7 +568,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     if (cta == 0) {  // ---- MMA issuer of the pair: the whole warp runs the loop and the waits, one elected lane issues
       // instruction descriptor: D fp32, A and B bf16, both K-major, N, M = 256 over the two CTAs
       const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((256u >> 4) << 24);
-      const uint64_t d_smem = umma_smem_desc(ptx::smem_u32(smem));  // byte offsets / 16 are added to its address field
+      const uint64_t d_smem = ptx::umma_smem_desc(ptx::smem_u32(smem));  // byte offsets / 16 are added to its address field
       uint32_t it = 0;
       bool ok = true;
       for (int t = 0; t < n_tiles && ok; ++t) {

@@ -198,8 +198,6 @@ static bool rope_frequencies(const sdlm_rope& r, int rot, double* freq, float* m
   return true;
 }
 
-static inline bool rope_a16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 }  // namespace sdlm
 
 using namespace sdlm;
@@ -217,8 +215,8 @@ extern "C" sdlm_status sdlm_qk_norm_rope(sdlm_ctx* ctx, int32_t batch, int32_t D
   if (n_heads2 == 0) {
     k = nullptr; k_out = nullptr; k_weight = nullptr; k_stride = 0;
   }
-  if (!rope_a16(q) || !rope_a16(q_out) || (q_weight && !rope_a16(q_weight))) return SDLM_ERR_INVALID_ARG;
-  if (k && (!rope_a16(k) || !rope_a16(k_out) || (k_weight && !rope_a16(k_weight)))) return SDLM_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(q_out) || (q_weight && !aligned16(q_weight))) return SDLM_ERR_INVALID_ARG;
+  if (k && (!aligned16(k) || !aligned16(k_out) || (k_weight && !aligned16(k_weight)))) return SDLM_ERR_INVALID_ARG;
   if (!(eps >= 0.f) || isinf(eps)) return SDLM_ERR_INVALID_ARG;
   const long long qw = (long long)n_heads * d, kw = (long long)n_heads2 * d;
   // (a stride of 2^40 elements is beyond any memory; the bound keeps the products below in 64 bits)

@@ -66,22 +66,6 @@ struct TreeParams {
 // Node of stacked row R (see inv_G).
 __device__ __forceinline__ int tree_node(const TreeParams& p, int R) { return p.inv_G ? (int)__umulhi((uint32_t)R, p.inv_G) : R; }
 
-__device__ __forceinline__ uint64_t tree_smem_desc(uint32_t saddr) {
-  // K-major operand, 128-byte swizzle, 8-row groups 1024 bytes apart; descriptor version 1 (sm_100)
-  return (uint64_t)((saddr & 0x3FFFF) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) |
-         ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
-
-// D (tensor memory) = or += A (tensor memory: 128 lanes, two bf16 of consecutive k per 32-bit column) * B (shared memory)
-__device__ __forceinline__ void tree_umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-
 // Largest of a thread's 64 scores (four chains), NaN left out; with EDGE only over the keys whose bit is set.
 template <bool EDGE>
 __device__ __forceinline__ float tree_row_max(const uint32_t (&x)[64], uint32_t lo, uint32_t hi) {
@@ -476,8 +460,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attn_kernel(const TreePa
       const int X = warp - 1;
       const uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | ((64u >> 3) << 17) | ((128u >> 4) << 24);
       const uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(HD >> 3) << 17) | ((128u >> 4) << 24);
-      const uint64_t d_q = tree_smem_desc(ptx::smem_u32(q_s)), d_kr = tree_smem_desc(ptx::smem_u32(k_ring)),
-                     d_vr = tree_smem_desc(ptx::smem_u32(v_ring));
+      const uint64_t d_q = ptx::umma_smem_desc(ptx::smem_u32(q_s)), d_kr = ptx::umma_smem_desc(ptx::smem_u32(k_ring)),
+                     d_vr = ptx::umma_smem_desc(ptx::smem_u32(v_ring));
       const uint32_t d_s = tmem_base + X * 128, d_o = tmem_base + O_COL + X * 128;
       bool ok = true;
       int slot_k = 0, slot_v = 0;
@@ -534,7 +518,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attn_kernel(const TreePa
           if (ptx::elect_one()) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              tree_umma_ts(d_o, d_p + k * 8, d_v + (uint64_t)((k * 32) >> 4), idesc_o, (tile > first || k) ? 1u : 0u);
+              ptx::umma_bf16_ts(d_o, d_p + k * 8, d_v + (uint64_t)((k * 32) >> 4), idesc_o, (tile > first || k) ? 1u : 0u);
             ptx::umma_commit(&pv_done[X * 2 + buf]);
             ptx::umma_commit(&v_free[slot_v]);
           }
@@ -871,13 +855,11 @@ cudaError_t setup_tree(sdlm_ctx* ctx) {
 
 using namespace sdlm;
 
-static inline bool tree_a16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 extern "C" sdlm_status sdlm_tree_attn(sdlm_ctx* ctx, int32_t batch, int32_t n, const int32_t* seq_ids, const int32_t* n_nodes,
                                       const int32_t* parent, const void* q, const void* k_tree, const void* v_tree,
                                       void* out, void* stream) {
   if (!ctx || !parent || !q || !k_tree || !v_tree || !out || batch < 1 || n < 1) return SDLM_ERR_INVALID_ARG;
-  if (!tree_a16(q) || !tree_a16(k_tree) || !tree_a16(v_tree) || !tree_a16(out)) return SDLM_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_tree) || !aligned16(v_tree) || !aligned16(out)) return SDLM_ERR_INVALID_ARG;
   if (batch > ctx->cfg.max_batch || n > kMaxTreeNodes) return SDLM_ERR_SHAPE;
   if (!(ctx->scale > 0.0f)) return SDLM_ERR_UNSUPPORTED;
   if (!same_device(ctx)) return SDLM_ERR_INVALID_ARG;
