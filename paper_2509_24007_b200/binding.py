@@ -841,7 +841,7 @@ class Sdlm:
     @_placed
     def kv_gather_batch(self, k_out: torch.Tensor, v_out: torch.Tensor, seq_ids: Optional[torch.Tensor] = None) -> None:
         """sdlm_kv_gather_batch: k_out / v_out [batch, length, Hkv, d]; rows beyond a slot's length stay as they are."""
-        if k_out.dim() != 4 or k_out.shape[2:] != (self.cfg.n_kv_heads, self.cfg.head_dim):
+        if not isinstance(k_out, torch.Tensor) or k_out.dim() != 4 or k_out.shape[2:] != (self.cfg.n_kv_heads, self.cfg.head_dim):
             raise ValueError("k_out and v_out must be [batch, length, Hkv, d]")
         gpu = self.device_index
         batch, length = k_out.shape[:2]
@@ -873,10 +873,10 @@ class Sdlm:
             _refuse(logits, logits.dtype, "logits", gpu)
         ins = [_is(u, f32, rows, "u", gpu), _is(temperature, f32, rows, "temperature", gpu), _is(top_k, i32, rows, "top_k", gpu),
                _is(top_p, f32, rows, "top_p", gpu), _is(min_p, f32, rows, "min_p", gpu)]
-        token = u.new_empty(shape, dtype=i32) if token is None else token
-        prob = u.new_empty(shape) if prob is None else prob
-        entropy = u.new_empty(shape) if entropy is None else entropy
-        n_kept = u.new_empty(shape, dtype=i32) if n_kept is None else n_kept
+        token = logits.new_empty(shape, dtype=i32) if token is None else token
+        prob = logits.new_empty(shape, dtype=f32) if prob is None else prob
+        entropy = logits.new_empty(shape, dtype=f32) if entropy is None else entropy
+        n_kept = logits.new_empty(shape, dtype=i32) if n_kept is None else n_kept
         code = self.lib.sdlm_sample(self.ctx, rows, V, LOGITS_F32 if logits.dtype is f32 else LOGITS_BF16, logits.data_ptr(), stride,
                                     *ins, _is(token, i32, rows, "token", gpu), _is(prob, f32, rows, "prob", gpu),
                                     _is(entropy, f32, rows, "entropy", gpu), _is(n_kept, i32, rows, "n_kept", gpu), _stream_ptr(None))

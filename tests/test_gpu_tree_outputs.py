@@ -148,3 +148,13 @@ def test_sampling_outputs_over_logits_parameters_and_each_other():
         same = f[param].clone()
         got = call(**{param: same, out: same})
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_missing_tensors_are_refused_by_name_of_the_call():
+    t = Tree(4, 2, 64, [10], 4, seed=55)
+    logits, u = torch.zeros((2, 64), device="cuda"), torch.zeros(2, device="cuda")
+    for call in (lambda: t.sd.sample(logits, None), lambda: t.sd.sample(None, u), lambda: t.sd.kv_gather_batch(None, None),
+                 lambda: t.sd.tree_attn(t.q, t.k, t.v, None), lambda: t.sd.tree_attn(t.q, None, t.v, t.parent),
+                 lambda: t.sd.tree_commit(None, t.parent, t.parent, t.k, t.v), lambda: t.sd.qk_norm_rope(None, t.k, pk.RopeConfig())):
+        with pytest.raises((TypeError, ValueError, pk.SdlmError)):
+            call()
