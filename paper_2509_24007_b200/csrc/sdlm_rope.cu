@@ -14,7 +14,7 @@
 // million times a frequency near 1 keeps no fraction worth having in 32 bits); the frequencies are worked out on the
 // host in 64 bits and travel as kernel arguments.  Everything else is fp32 with one rounding to bf16 at the end.
 //
-// 16381 rows of 40 + 8 heads of 128 (403 MB): 70.6 us, 5.7 TB/s; 672 rows of 16 + 2 heads: 4.4 us; one row: 2.8 us, which
+// 16381 rows of 40 + 8 heads of 128 (403 MB): 73 us, 5.5 TB/s; 672 rows of 16 + 2 heads: 4.3 us; one row: 2.8 us, which
 // is a launch.
 #include "sdlm_internal.h"
 #include "sdlm_ptx.cuh"

@@ -22,10 +22,11 @@
 //      (all tokens that a small top-k can keep are, and then only the list is looked at: top-k of 50 and top-p 88 -> 76 us);
 //   5. without top-p one pass forms the kept weights; every thread block then knows the weight of all slices, and the one
 //      that holds u W finds its token.
-// Rows of 151936 bf16 logits, 1 / 128 / 256 of them: greedy 9 / 22 / 41 us (128: 1.8 TB/s, loads that two thread blocks an
-// SM have in flight), all tokens kept 12 / 58 / 103, top-k of 50 16 / 51 / 99, top-p of 0.9 that keeps tens of thousands
-// of tokens 38 / 147 / 264.  A pass over all weights (14 64-bit operations a token, 61 a clock and SM) is 35 of those 58;
-// top-p takes one to two of them, and the thread blocks of a row wait for each other five to eight times.
+// Rows of 151936 bf16 logits, 1 / 128 / 256 of them, in a graph over three sets of them: greedy 9 / 36 / 60 us (128: 1.1 TB/s),
+// all tokens kept 13 / 65 / 112, top-k of 50 17 / 69 / 118, that and top-p of 0.9 29 / 86 / 155, top-p alone, which keeps
+// tens of thousands of tokens, 39 / 154 / 275; on one set, which stays in L2, 4 to 8 us less.  A pass over all weights (14
+// 64-bit operations a token, 61 a clock and SM) is some 30 of those 65; top-p takes one to two of them, and the thread blocks
+// of a row wait for each other five to eight times.
 // -inf and NaN fail every comparison below, so they need no mask of their own.
 //
 // The answer is a comparison of sums of up to 2^18 weights with u W or p times their total, and a token changes when a

@@ -22,9 +22,11 @@
 // registers (no exchange between threads), stages queries and writes rows out.  Only key tiles that are not seen whole
 // look at the row's 64-bit visibility word.
 //
-// Measured (16 query and 2 KV heads of 128 where not said otherwise): one sequence of 1024, one node: 12.8 us; 32
-// sequences of 512..4096, 13 nodes (80 MB): 30 us, 2.7 TB/s; 8 of 32768, 32 nodes: 89 us, 3.0 TB/s and 0.77 PFLOP/s; 64 of
-// 512..4096, 64 nodes, 40 and 8 heads: 270 us, 2.5 TB/s and 0.56 PFLOP/s.  What bounds it is the round of a key tile
+// Measured in a graph over three sets of inputs at 1965 MHz (16 query and 2 KV heads of 128 where not said otherwise): one
+// sequence of 1024, one node: 12.9 us; 32 sequences of 512..4096, 13 nodes (80 MB): 34 us, 2.3 TB/s (30 on one set, which
+// stays in L2); 8 of 32768, 32 nodes: 89 us, 3.0 TB/s and 0.77 PFLOP/s; 64 of 512..4096, 64 nodes, 40 and 8 heads: 270 to 284
+// us, 2.5 TB/s and 0.55 PFLOP/s.  Called for seconds the last two take 102 and 305 us, at the 1.67 to 1.8 GHz the power cap
+// leaves.  Heads of 64 (4 over 2): 32 of 512..4096, 13 nodes 24 us, 64 of 4096, 64 nodes 57 us.  What bounds it is the round of a key tile
 // between an issuer and its softmax group (S ready, scores read, weights written, P V issued): about half of the time
 // goes into its waits and barriers, with all arithmetic taken out the third case still takes 44 us.
 #include "sdlm_internal.h"
