@@ -228,12 +228,13 @@ struct SampleRow {
   }
   __device__ __forceinline__ SampleWeight weight(float v) const { return sample_weight(v, v_floor, (double)vmax, scale); }
 
-  // Bounds of the weight of n tokens of bin b, as multiples of 2^-40 rounded outwards.  The factors 1 -+ 1e-5 cover what
-  // rounding the distance, which is up to the bin's number, and the powers of two may be off by.
+  // Bounds of the weight of n tokens of bin b, as multiples of 2^-40 rounded outwards.  The factors 1 -+ 2e-5 cover four
+  // roundings: of the distance (two of 2^-24 of at most 2047 bins, a bin being 0.0098: 2.4e-6), of the exponent here (2^-24
+  // of at most 28.9: 1.2e-6), of exp2f and the product (3e-7), and of each weight to 2^-45 (half of it against e^-20: 6.9e-6).
   __device__ __forceinline__ void bounds(int b, uint32_t n, uint64_t& lo, uint64_t& hi) const {
     const double kappa = scale / (double)bin_scale;  // log2 units a bin
-    const float near = b == 0 ? 1.0f : exp2f((float)(-((double)b - 0.5) * kappa)) * 1.00001f;
-    const float far = b == kSampleBins - 1 ? 0.0f : exp2f((float)(-((double)b + 0.5) * kappa)) * 0.99999f;
+    const float near = b == 0 ? 1.0f : exp2f((float)(-((double)b - 0.5) * kappa)) * 1.00002f;
+    const float far = b == kSampleBins - 1 ? 0.0f : exp2f((float)(-((double)b + 0.5) * kappa)) * 0.99998f;
     lo = (uint64_t)((double)n * (double)far * 1099511627776.0);
     hi = n ? (uint64_t)((double)n * (double)near * 1099511627776.0) + 1u : 0u;
   }
